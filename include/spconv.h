@@ -52,7 +52,12 @@ typedef enum {
     SPCONV_E_HIP = 6          /* a HIP runtime call failed (message names it) */
 } spconv_status;
 
-typedef enum { SPCONV_F32 = 0, SPCONV_F16 = 1 } spconv_dtype;
+typedef enum {
+    SPCONV_F32 = 0,
+    SPCONV_F16 = 1,
+    SPCONV_BF16 = 2, /* the operators of 8-bit products, routing and experts only */
+    SPCONV_FP8 = 3   /* 8-bit e4m3 codes with scales (below); as BF16, and only where a call says so */
+} spconv_dtype;
 
 typedef enum { SPCONV_ACT_NONE = 0, SPCONV_ACT_RELU = 1, SPCONV_ACT_RELU6 = 2 } spconv_act;
 
@@ -268,6 +273,74 @@ SPCONV_API spconv_status spconv_plan_create_dense_blocked(spconv_plan *out, int3
                                                           const float *dense, int32_t block_rows,
                                                           int32_t block_cols, const float *bias, spconv_act act,
                                                           spconv_dtype storage);
+
+/* ---------------------------------------------------------------------------
+ * Dense layers in 8-bit floating point, with a 32-bit scale for each block.
+ *
+ * The 8-bit form of a row-major matrix [rows][cols] is a code array and a
+ * scale array.  With kb = ceil(cols / 128):
+ *   codes   [rows][128 * kb] bytes, OCP e4m3 (largest value 448); zeros past
+ *           cols; 16-byte aligned
+ *   scales  floats, one for each 128 columns of a row, [kb][rows] (the form of
+ *           activations), or one for each 128 x 128 block,
+ *           [ceil(rows / 128)][kb] (the form of weights)
+ * An element's value is its code's value times its block's scale.
+ *
+ * These calls launch asynchronously on `stream` (NULL: the default stream) of
+ * the current device, allocate nothing and never synchronize.  Device pointers
+ * must be aligned to their element size; 16-byte alignment of x, y and of x's
+ * row stride takes the fastest load path.  Outputs and workspaces must not
+ * overlap inputs or each other (SPCONV_E_ARG).
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Quantise: with a = max(max |x| over the block, 2^-100), scale = a / 448 and
+ * code = x * (448 / a) rounded to the nearest e4m3 value, ties to even; every
+ * step in fp32.  A block that holds an infinity or a NaN gets that as its
+ * scale, so that every product with it is NaN.
+ *   x           device, [rows][cols] of dtype (F32, F16 or BF16), row stride ldx >= cols elements
+ *   block_rows  1 (activations) or 128 (weights)
+ *   q, scale    out, in the form above
+ * rows == 0 or cols == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
+ * cols, bad dtype or alignment, overlap), SPCONV_E_UNSUPPORTED (block_rows not
+ * 1 or 128), SPCONV_E_SHAPE (rows * ceil(cols / 128) of 2^27 or more, cols
+ * above 2^30), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_quantize_fp8(const void *x, spconv_dtype dtype, int64_t ldx, int32_t rows,
+                                             int32_t cols, int32_t block_rows, void *q, float *scale, void *stream);
+
+/*
+ * Dense layer with an 8-bit weight:
+ *   y[t][r] = act( bias[r] + sum_c value(x[t][c]) * value(w[r][c]) )
+ * The codes' products over each block of 128 input channels are summed on the
+ * matrix cores in fp32 and scaled in fp32; the sum over blocks, the bias and
+ * the activation are fp32, rounded once to y's type.
+ *   x           device, n rows of cin channels: x_dtype F32, F16 or BF16 with a
+ *               row stride of ldx >= cin elements, quantised here as by
+ *               spconv_quantize_fp8 with block_rows = 1; or FP8 codes (ldx unused)
+ *   x_scale     the scales of FP8 codes, [kb][n]; NULL for other types
+ *   w, w_scale  the weight [cout][cin] in 8-bit form, 128 x 128 blocks
+ *   bias        device, cout floats, or NULL
+ *   y           device, [n][cout] of y_dtype (F32, F16 or BF16)
+ *   workspace   device, 16-byte aligned, of at least the size that
+ *               spconv_linear_fp8_workspace gives (NULL where that is 0); its
+ *               contents mean nothing before or after the call's work
+ * n == 0 or cout == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
+ * cin, bad dtype, act or alignment, x_scale missing or not asked for, workspace
+ * too small, overlap), SPCONV_E_SHAPE (cin == 0 with outputs, cin above 2^24, n
+ * * ceil(cin / 128) of 2^27 or more, n * cout of 2^36 or more), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx, const float *x_scale,
+                                           const void *w, const float *w_scale, const float *bias, spconv_act act,
+                                           void *y, spconv_dtype y_dtype, int32_t n, int32_t cin, int32_t cout,
+                                           void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace for such a call, host only.  Errors: SPCONV_E_ARG (NULL,
+ * negative size, bad dtype), SPCONV_E_SHAPE as above. */
+SPCONV_API spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout,
+                                                     int64_t *bytes);
 
 /* ---------------------------------------------------------------------------
  * Planner controls and introspection.  These let a caller (and the CPU-only

@@ -21,6 +21,8 @@ from .spconv import (  # noqa: F401
     spconv_detect_blocks,
     spconv_last_error,
     spconv_linear,
+    spconv_linear_fp8,
+    spconv_linear_fp8_workspace,
     spconv_options_init,
     spconv_plan_create,
     spconv_plan_create_blocked,
@@ -38,5 +40,10 @@ from .spconv import (  # noqa: F401
     spconv_plan_check,
     spconv_plan_set_wait_limit,
     SPCONV_FLAG_WAIT_GAVE_UP,
+    spconv_quantize_fp8,
     spconv_run,
+)
+from .experts import (  # noqa: F401
+    Fp8Linear,
+    quantize_fp8,
 )

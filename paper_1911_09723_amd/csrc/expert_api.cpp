@@ -1,0 +1,202 @@
+// C ABI of the 8-bit products, the router and the experts (declared in
+// include/spconv.h): argument checks, then asynchronous launches on the
+// caller's stream.  Nothing is allocated and nothing synchronizes.
+#include "spconv.h"
+
+#include <hip/hip_runtime_api.h>
+
+#include <limits>
+
+#include "expert_ops.hpp"
+#include "status.hpp"
+
+namespace {
+
+using spconv::blocks_of;
+using spconv::set_error;
+
+constexpr int64_t kMostBlocks = int64_t(1) << 27;  // row blocks of a matrix: launches stay below 2^32 threads
+constexpr int64_t kMostOutputs = int64_t(1) << 36;
+constexpr int32_t kMostChannels = 1 << 24;
+
+bool is_float(int32_t type) { return type == SPCONV_F32 || type == SPCONV_F16 || type == SPCONV_BF16; }
+int64_t size_of(int32_t type) { return type == SPCONV_F32 ? 4 : type == SPCONV_FP8 ? 1 : 2; }
+bool aligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(to) == 0; }
+
+struct Range {
+    const void *p;
+    int64_t bytes;
+};
+
+bool overlap(Range a, Range b) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && a.bytes > 0 && b.bytes > 0 && a0 < b0 + static_cast<uintptr_t>(b.bytes) &&
+           b0 < a0 + static_cast<uintptr_t>(a.bytes);
+}
+
+// Whether an output overlaps an input or another output.
+template <int OUT, int IN>
+bool outputs_overlap(const Range (&out)[OUT], const Range (&in)[IN]) {
+    for (int i = 0; i < OUT; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j]))
+                return true;
+        for (int j = 0; j < IN; ++j)
+            if (overlap(out[i], in[j]))
+                return true;
+    }
+    return false;
+}
+
+// Bytes that strided rows span; the caller keeps the product in range.
+int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t size) { return rows ? ((rows - 1) * ld + cols) * size : 0; }
+constexpr int64_t kMostStride = int64_t(1) << 34;
+
+int64_t code_bytes(int64_t rows, int64_t cols) { return rows * blocks_of(cols) * 128; }
+int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
+
+void clamp_of(spconv_act act, float &lo, float &hi) {
+    lo = act == SPCONV_ACT_NONE ? -std::numeric_limits<float>::infinity() : 0.0f;
+    hi = act == SPCONV_ACT_RELU6 ? 6.0f : std::numeric_limits<float>::infinity();
+}
+
+spconv_status launched(hipError_t e) { return e == hipSuccess ? SPCONV_OK : spconv::set_hip_error("kernel launch", e); }
+
+// Sizes of a linear layer; SPCONV_OK also where there is nothing to do.
+spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
+    if (!is_float(x_dtype) && x_dtype != SPCONV_FP8)
+        return set_error(SPCONV_E_ARG, "x_dtype must be SPCONV_F32, _F16, _BF16 or _FP8");
+    if (n < 0 || cin < 0 || cout < 0)
+        return set_error(SPCONV_E_ARG, "n, cin and cout must be >= 0");
+    if (n == 0 || cout == 0)
+        return SPCONV_OK;
+    if (cin == 0)
+        return set_error(SPCONV_E_SHAPE, "cin must be >= 1");
+    if (cin > kMostChannels || cout > kMostChannels)
+        return set_error(SPCONV_E_SHAPE, "cin and cout must be at most 2^24");
+    if (static_cast<int64_t>(n) * blocks_of(cin) >= kMostBlocks)
+        return set_error(SPCONV_E_SHAPE, "n * ceil(cin / 128) must be below 2^27");
+    if (static_cast<int64_t>(n) * cout >= kMostOutputs)
+        return set_error(SPCONV_E_SHAPE, "n * cout must be below 2^36");
+    return SPCONV_OK;
+}
+
+// Rows that the product's kernel does not quantise itself go through the workspace: codes, then scales.
+int64_t linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
+    if (x_dtype == SPCONV_FP8 || n == 0 || cout == 0 || spconv::linear_takes_rows(n, cin, cout))
+        return 0;
+    return code_bytes(n, cin) + align16(static_cast<int64_t>(n) * blocks_of(cin) * 4);
+}
+
+}  // namespace
+
+extern "C" {
+
+spconv_status spconv_quantize_fp8(const void *x, spconv_dtype dtype, int64_t ldx, int32_t rows, int32_t cols,
+                                  int32_t block_rows, void *q, float *scale, void *stream) {
+    spconv::clear_error();
+    if (!is_float(dtype))
+        return set_error(SPCONV_E_ARG, "dtype must be SPCONV_F32, _F16 or _BF16");
+    if (rows < 0 || cols < 0)
+        return set_error(SPCONV_E_ARG, "rows and cols must be >= 0");
+    if (block_rows != 1 && block_rows != 128)
+        return set_error(SPCONV_E_UNSUPPORTED, "block_rows must be 1 or 128");
+    if (rows == 0 || cols == 0)
+        return SPCONV_OK;
+    if (!x || !q || !scale)
+        return set_error(SPCONV_E_ARG, "x, q or scale is NULL");
+    if (ldx < cols)
+        return set_error(SPCONV_E_ARG, "ldx must be at least cols");
+    const int64_t kb = blocks_of(cols);
+    if (cols > (1 << 30) || ldx > kMostStride || rows * kb >= kMostBlocks)
+        return set_error(SPCONV_E_SHAPE, "rows * ceil(cols / 128) must be below 2^27, cols at most 2^30, ldx at most 2^34");
+    if (!aligned(x, size_of(dtype)) || !aligned(scale, 4) || !aligned(q, 16))
+        return set_error(SPCONV_E_ARG, "x and scale must be aligned to their element size, q to 16 bytes");
+    const Range in[] = {{x, span(rows, cols, ldx, size_of(dtype))}};
+    const Range out[] = {{q, code_bytes(rows, cols)}, {scale, (block_rows == 1 ? rows : blocks_of(rows)) * kb * 4}};
+    if (outputs_overlap(out, in))
+        return set_error(SPCONV_E_ARG, "x, q and scale must not overlap");
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *codes = static_cast<uint8_t *>(q);
+    return launched(block_rows == 1 ? spconv::launch_quantize_rows(x, dtype, ldx, rows, cols, codes, scale, s)
+                                    : spconv::launch_quantize_blocks(x, dtype, ldx, rows, cols, codes, scale, s));
+}
+
+spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout, int64_t *bytes) {
+    spconv::clear_error();
+    if (!bytes)
+        return set_error(SPCONV_E_ARG, "bytes is NULL");
+    *bytes = 0;
+    const spconv_status st = check_linear(x_dtype, n, cin, cout);
+    if (st == SPCONV_OK)
+        *bytes = linear_workspace(x_dtype, n, cin, cout);
+    return st;
+}
+
+spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx, const float *x_scale, const void *w,
+                                const float *w_scale, const float *bias, spconv_act act, void *y, spconv_dtype y_dtype,
+                                int32_t n, int32_t cin, int32_t cout, void *workspace, int64_t workspace_bytes,
+                                void *stream) {
+    spconv::clear_error();
+    const spconv_status st = check_linear(x_dtype, n, cin, cout);
+    if (st != SPCONV_OK)
+        return st;
+    if (!is_float(y_dtype))
+        return set_error(SPCONV_E_ARG, "y_dtype must be SPCONV_F32, _F16 or _BF16");
+    if (act < SPCONV_ACT_NONE || act > SPCONV_ACT_RELU6)
+        return set_error(SPCONV_E_ARG, "act must be SPCONV_ACT_NONE, _RELU or _RELU6");
+    if (n == 0 || cout == 0)
+        return SPCONV_OK;
+    if (!x || !w || !w_scale || !y)
+        return set_error(SPCONV_E_ARG, "x, w, w_scale or y is NULL");
+    const bool codes = x_dtype == SPCONV_FP8;
+    if (codes != (x_scale != nullptr))
+        return set_error(SPCONV_E_ARG, "x_scale belongs to SPCONV_FP8 rows, and to them only");
+    if (!codes && ldx < cin)
+        return set_error(SPCONV_E_ARG, "ldx must be at least cin");
+    if (!codes && ldx > kMostStride)
+        return set_error(SPCONV_E_SHAPE, "ldx must be at most 2^34");
+    if (!aligned(x, codes ? 16 : size_of(x_dtype)) || !aligned(w, 16) || !aligned(y, size_of(y_dtype)) ||
+        !aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(workspace, 16))
+        return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size, codes and the workspace to 16 bytes");
+    const int64_t kb = blocks_of(cin), need = linear_workspace(x_dtype, n, cin, cout);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return set_error(SPCONV_E_ARG, "the workspace is smaller than spconv_linear_fp8_workspace says");
+    const Range in[] = {{x, codes ? code_bytes(n, cin) : span(n, cin, ldx, size_of(x_dtype))},
+                        {x_scale, kb * n * 4},
+                        {w, code_bytes(cout, cin)},
+                        {w_scale, blocks_of(cout) * kb * 4},
+                        {bias, static_cast<int64_t>(cout) * 4}};
+    const Range out[] = {{y, static_cast<int64_t>(n) * cout * size_of(y_dtype)}, {workspace, need}};
+    if (outputs_overlap(out, in))
+        return set_error(SPCONV_E_ARG, "y and the workspace must not overlap each other or an input");
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    spconv::LinearArgs a{};
+    a.x = x;
+    a.ldx = ldx;
+    a.xs = x_scale;
+    a.w = static_cast<const uint8_t *>(w);
+    a.ws = w_scale;
+    a.bias = bias;
+    a.y = y;
+    a.x_type = x_dtype;
+    a.y_type = y_dtype;
+    a.n = n;
+    a.cin = cin;
+    a.cout = cout;
+    a.kb = static_cast<int32_t>(kb);
+    clamp_of(act, a.lo, a.hi);
+    if (need > 0) {
+        uint8_t *q = static_cast<uint8_t *>(workspace);
+        float *scale = reinterpret_cast<float *>(q + code_bytes(n, cin));
+        const hipError_t e = spconv::launch_quantize_rows(x, x_dtype, ldx, n, cin, q, scale, s);
+        if (e != hipSuccess)
+            return launched(e);
+        a.x = q;
+        a.xs = scale;
+        a.x_type = spconv::kFp8;
+    }
+    return launched(spconv::launch_linear_fp8(a, s));
+}
+
+}  // extern "C"

@@ -1,0 +1,188 @@
+// y = clamp(x W^T + b) for a weight in 8 bits with a scale for each 128 x 128
+// block and rows with a scale for each 128 channels (fp8.hpp, fp8_product.hpp).
+#include <algorithm>
+
+#include "expert_ops.hpp"
+#include "fp8_product.hpp"
+
+namespace spconv {
+namespace {
+
+constexpr int kXcds = 8;
+
+__device__ __forceinline__ f4 bias4(const float *bias, int32_t ch, int32_t cout) {
+    f4 v{0, 0, 0, 0};
+    if (bias)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = ch + i < cout ? bias[ch + i] : 0.0f;
+    return v;
+}
+
+__device__ __forceinline__ void finish(const LinearArgs &a, bool wide, int32_t row, int32_t ch, f4 v) {
+    if (row >= a.n || ch >= a.cout)
+        return;
+    v += bias4(a.bias, ch, a.cout);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = clamp_to(v[i], a.lo, a.hi);
+    store4(a.y, a.y_type, static_cast<int64_t>(row) * a.cout + ch, v, a.cout - ch, wide);
+}
+
+template <class S, bool EXACT>
+__global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t ctiles, int32_t ttiles, bool wide) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // neighbouring tiles on one XCD, in groups of 8 row tiles: they share W and X in its L2
+    const int32_t per = gridDim.x / kXcds, id = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    if (id >= ctiles * ttiles)
+        return;
+    const int32_t group = id / (8 * ctiles), high = min(8, ttiles - 8 * group), in = id - group * 8 * ctiles;
+    const int32_t ct = in / high, tt = group * 8 + in - ct * high;
+    const int32_t c0 = ct * S::BC, t0 = tt * S::BT;
+    const int64_t pitch = static_cast<int64_t>(a.kb) * kBlock;
+    const uint8_t *src[S::kLoads];
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const int line = tile_line<S>(wave, lane, i);
+        // lines past the last row or channel repeat it: their results are not stored
+        const uint8_t *row = line < S::BC ? a.w + min(c0 + line, a.cout - 1) * pitch
+                                          : static_cast<const uint8_t *>(a.x) + min(t0 + line - S::BC, a.n - 1) * pitch;
+        src[i] = row + tile_byte(line, lane);
+    }
+    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int32_t cw = c0 + wc * S::NC * 16;
+    const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
+    const float *xs = a.xs + min(t0 + wave * 64 + lane, a.n - 1);
+    f4 acc[S::NC][S::NT] = {};
+    tile_product<S, EXACT, false>(acc, src, xs, a.n, ws, nullptr, a.kb, lds, wave, lane);
+#pragma unroll
+    for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+        for (int t = 0; t < S::NT; ++t)
+            finish(a, wide, t0 + (wt * S::NT + t) * 16 + (lane & 15), cw + c * 16 + (lane >> 4) * 4, acc[c][t]);
+}
+
+// XT: Fp8 (codes) or the type of rows that are quantised here.
+template <typename XT, int TT, int CT, int U>
+__global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x, bool wide) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int32_t c0 = blockIdx.x * 16 * CT, t0 = blockIdx.y * 16 * TT;
+    const int64_t pitch = static_cast<int64_t>(a.kb) * kBlock;
+    const uint8_t *w[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+        w[c] = a.w + min(c0 + c * 16 + (lane & 15), a.cout - 1) * pitch;
+    const float *ws = a.ws + static_cast<int64_t>(c0 / kBlock) * a.kb;
+    int32_t row[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+        row[t] = min(t0 + t * 16 + (lane & 15), a.n - 1);
+    f4 acc[CT * TT] = {};
+    for (int32_t b0 = wave; b0 < a.kb; b0 += waves * U) {
+        i8 wf[U][CT];
+        RowPart xp[U][TT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.kb - 1);
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                wf[u][c] = weight_part(w[c], b, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.kb - 1);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                if constexpr (sizeof(XT) == 1)
+                    xp[u][t] = row_codes(static_cast<const uint8_t *>(a.x) + row[t] * pitch,
+                                         a.xs + static_cast<int64_t>(b) * a.n + row[t], b, lane);
+                else
+                    xp[u][t] = row_quantized(static_cast<const XT *>(a.x) + row[t] * a.ldx, b, a.cin, wide_x, lane);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (b0 + u * waves >= a.kb)
+                break;
+            const float sw = ws[b0 + u * waves];
+            Halves wh[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                wh[c] = halves(wf[u][c]);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const Halves xh = halves(xp[u][t].code);
+                const float s = xp[u][t].scale * sw;
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const f4 p = mfma128(wh[c], xh);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[c * TT + t][i] = fmaf(s, p[i], acc[c * TT + t][i]);
+                }
+            }
+        }
+    }
+    sum_waves<CT * TT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int i, f4 sum) {
+        finish(a, wide, t0 + i % TT * 16 + (lane & 15), c0 + i / TT * 16 + (lane >> 4) * 4, sum);
+    });
+}
+
+constexpr int32_t kStreamRows = 64;     // most rows that take the stream kernel
+constexpr int32_t kStreamQuantize = 16; // most rows that it quantises itself
+
+size_t size_of(int32_t type) { return type == kF32 ? 4 : type == kFp8 ? 1 : 2; }
+
+template <typename XT, int TT>
+hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_t stream) {
+    const int waves = std::min(a.kb, TT == 4 ? 8 : 16);
+    const dim3 grid((a.cout + 15) / 16, (a.n + 16 * TT - 1) / (16 * TT));
+    const size_t lds = static_cast<size_t>(waves) * TT * 1024;
+    if (a.kb > waves)
+        linear_stream<XT, TT, 1, 2><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+    else
+        linear_stream<XT, TT, 1, 1><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+    return hipGetLastError();
+}
+
+template <class S, bool EXACT>
+hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream) {
+    const int64_t ct = (a.cout + S::BC - 1) / S::BC, tt = (a.n + S::BT - 1) / S::BT;
+    static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void *>(linear_tile<S, EXACT>),
+                                                        hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    if (ready != hipSuccess)
+        return ready;
+    const int64_t grid = (ct * tt + kXcds - 1) / kXcds * kXcds;
+    linear_tile<S, EXACT><<<static_cast<uint32_t>(grid), S::kThreads, S::kLds, stream>>>(
+        a, static_cast<int32_t>(ct), static_cast<int32_t>(tt), wide);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) { return n <= kStreamQuantize; }
+
+hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
+    const bool wide_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size_of(a.x_type) % 16 == 0;
+    const bool wide = a.cout % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
+    if (a.x_type != kFp8)
+        return a.x_type == kF32   ? stream_launch<float, 1>(a, wide_x, wide, stream)
+               : a.x_type == kF16 ? stream_launch<_Float16, 1>(a, wide_x, wide, stream)
+                                  : stream_launch<__bf16, 1>(a, wide_x, wide, stream);
+    if (a.n <= 16)
+        return stream_launch<Fp8, 1>(a, wide_x, wide, stream);
+    if (a.n <= 32)
+        return stream_launch<Fp8, 2>(a, wide_x, wide, stream);
+    if (a.n <= kStreamRows)
+        return stream_launch<Fp8, 4>(a, wide_x, wide, stream);
+    if (a.y_type == kF32)
+        return tile_launch<TileShape<128, 128, 2, 2>, true>(a, wide, stream);
+    if (static_cast<int64_t>((a.cout + 255) / 256) * ((a.n + 255) / 256) >= 192)
+        return tile_launch<TileShape<256, 256, 2, 4>, false>(a, wide, stream);
+    return tile_launch<TileShape<128, 128, 2, 2>, false>(a, wide, stream);
+}
+
+}  // namespace spconv

@@ -1,0 +1,181 @@
+// The two product cores of 8-bit rows and weights (fp8.hpp): a tile of
+// channels x rows staged through LDS, and a few rows against weights that are
+// read once.  Both compute, for channels r (rows of W) and rows t of X,
+//
+//     sum over blocks b of  sx[b][t] * sw[r / 128][b] * (Wq[r] . Xq[t] over block b)
+//
+// One 8-bit matrix instruction spans exactly one block of 128 channels, so its result
+// is a block's sum and is added to the 32-bit accumulator with one fused
+// multiply-add by the block's scale (the exact form, fp8.hpp: four instructions
+// of 32 channels).  W is the instruction's row operand: a
+// lane then holds one row of X (one scale) and four neighbouring channels.
+#pragma once
+
+#include "fp8.hpp"
+
+namespace spconv {
+
+// ---------------------------------------------------------------------------
+// Tile core.  BC channels x BT rows, WC x WT wavefronts, each NC x NT pieces of
+// 16 x 16.  Per block of 128 channels, BC + BT lines of 128 bytes and BT scales
+// go straight from global memory to LDS (16 bytes a lane, no registers between),
+// into the other of two buffers while the products of this one run.
+//
+// A line's 16-byte pieces are stored in the order piece ^ (line / 2 % 8): 16
+// lanes that read one piece of 16 neighbouring lines then touch each of LDS's
+// 16-byte columns (256 bytes, two lines) once.  The permutation is done by the
+// loads' global addresses, within a line, since their LDS places are fixed.
+// ---------------------------------------------------------------------------
+template <int BC_, int BT_, int WC_, int WT_>
+struct TileShape {
+    static constexpr int BC = BC_, BT = BT_, WC = WC_, WT = WT_;
+    static constexpr int kWaves = WC * WT, kThreads = 64 * kWaves;
+    static constexpr int NC = BC / WC / 16, NT = BT / WT / 16;
+    static constexpr int kLines = BC + BT;
+    static constexpr int kLoads = kLines / 8 / kWaves;  // 8 lines an instruction
+    static constexpr int kStage = kLines * kBlock + BT * 4;
+    static constexpr int kLds = 2 * kStage;
+    static_assert(kLines % (8 * kWaves) == 0 && BT % 64 == 0 && BT / 64 <= kWaves, "whole loads a wavefront");
+};
+
+__device__ __forceinline__ void to_lds(const void *from, unsigned char *lds) {
+    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(const_cast<void *>(from)),
+                                     (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+}
+
+__device__ __forceinline__ void to_lds4(const void *from, unsigned char *lds) {
+    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(const_cast<void *>(from)),
+                                     (__attribute__((address_space(3))) void *)lds, 4, 0, 0);
+}
+
+// The line (0 .. BC + BT - 1, W's first) and the byte in it that this lane
+// copies with its i-th load.
+template <class S>
+__device__ __forceinline__ int tile_line(int wave, int lane, int i) {
+    return (wave + i * S::kWaves) * 8 + (lane >> 3);
+}
+__device__ __forceinline__ int tile_byte(int line, int lane) { return ((lane & 7) ^ (line >> 1 & 7)) * 16; }
+
+// acc[c][t] += the products over kb blocks.  src[i]: this lane's i-th line at
+// its byte, block 0; xs: this lane's row scale of block 0 (wavefronts below
+// BT / 64 only), xs_step floats from block to block; ws0, ws1: the scales by
+// block of the first and of the second half of the wavefront's channel pieces.
+template <class S, bool EXACT, bool HALVES>
+__device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const uint8_t *(&src)[S::kLoads],
+                                             const float *xs, int64_t xs_step, const float *ws0, const float *ws1,
+                                             int32_t kb, unsigned char *lds, int wave, int lane) {
+    const int wc = wave / S::WT, wt = wave % S::WT;
+    auto stage = [&](int32_t b, unsigned char *buf) {
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i)
+            to_lds(src[i] + static_cast<int64_t>(b) * kBlock, buf + (wave + i * S::kWaves) * 1024);
+        if (wave < S::BT / 64)
+            to_lds4(xs + b * xs_step, buf + S::kLines * kBlock + wave * 256);
+    };
+    // this lane's place in a piece of 16 lines: line lane % 16, 16-byte piece lane / 16 (and 4 further)
+    const int at = (lane & 15) * kBlock + (((lane >> 4) ^ ((lane & 15) >> 1)) * 16);
+    stage(0, lds);
+    __syncthreads();
+    for (int32_t b = 0; b < kb; ++b) {
+        const unsigned char *buf = lds + (b & 1) * S::kStage;
+        if (b + 1 < kb)
+            stage(b + 1, lds + (b + 1 & 1) * S::kStage);
+        const unsigned char *wl = buf + wc * S::NC * 16 * kBlock;
+        const unsigned char *xl = buf + (S::BC + wt * S::NT * 16) * kBlock;
+        const float *sl = reinterpret_cast<const float *>(buf + S::kLines * kBlock) + wt * S::NT * 16 + (lane & 15);
+        const float sw0 = ws0[b], sw1 = HALVES ? ws1[b] : 0.0f;
+        decltype(operand<EXACT>(i8{})) xf[S::NT];
+        float s0[S::NT], s1[S::NT];
+#pragma unroll
+        for (int t = 0; t < S::NT; ++t) {
+            xf[t] = operand<EXACT>(join(*reinterpret_cast<const u4 *>(xl + t * 16 * kBlock + at),
+                                        *reinterpret_cast<const u4 *>(xl + t * 16 * kBlock + (at ^ 64))));
+            s0[t] = sl[t * 16] * sw0;
+            s1[t] = sl[t * 16] * sw1;
+        }
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) {
+            const auto wf = operand<EXACT>(join(*reinterpret_cast<const u4 *>(wl + c * 16 * kBlock + at),
+                                                *reinterpret_cast<const u4 *>(wl + c * 16 * kBlock + (at ^ 64))));
+#pragma unroll
+            for (int t = 0; t < S::NT; ++t) {
+                const f4 p = mfma128(wf, xf[t]);
+                const float s = HALVES && c >= S::NC / 2 ? s1[t] : s0[t];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[c][t][i] = fmaf(s, p[i], acc[c][t][i]);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Stream core: up to 16 TT rows against CT pieces of 16 channels, the blocks
+// of the input channels dealt to the wavefronts of a workgroup in turn.
+// Nothing is shared between wavefronts but the final sum, so operands go from
+// global memory (rows: from L2) to registers in the instruction's layout.  What
+// bounds it is the weight's bytes, so the products are the exact ones.
+// ---------------------------------------------------------------------------
+
+// A lane's part (32 of 128 channels) of one row and block, and the block's scale.
+struct RowPart {
+    i8 code;
+    float scale;
+};
+
+// Rows kept as codes.
+__device__ __forceinline__ RowPart row_codes(const uint8_t *row, const float *scale, int32_t b, int lane) {
+    const uint8_t *p = row + static_cast<int64_t>(b) * kBlock + (lane >> 4) * 16;
+    return {join(*reinterpret_cast<const u4 *>(p), *reinterpret_cast<const u4 *>(p + 64)), *scale};
+}
+
+// Rows in f32, f16 or bf16, quantised here: the four lanes of a row hold the
+// whole block between them.
+template <typename T>
+__device__ __forceinline__ RowPart row_quantized(const T *row, int32_t b, int32_t cols, bool wide, int lane) {
+    const int32_t c = b * kBlock + (lane >> 4) * 16;
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int32_t at = c + (i >> 1) * 64 + (i & 1) * 8;
+        load8_tail(row + at, cols - at, wide, v[i]);
+    }
+    uint32_t m = max(max(most8(v[0]), most8(v[1])), max(most8(v[2]), most8(v[3])));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
+    const Scale s = scale_of(m);
+    i8 code;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        code[2 * i] = static_cast<int>(codes4(v[i], s.inv));
+        code[2 * i + 1] = static_cast<int>(codes4(v[i] + 4, s.inv));
+    }
+    return {code, s.scale};
+}
+
+// A lane's part of one piece of 16 weight rows and block b; `row`: its row.
+__device__ __forceinline__ i8 weight_part(const uint8_t *row, int32_t b, int lane) {
+    const uint8_t *p = row + static_cast<int64_t>(b) * kBlock + (lane >> 4) * 16;
+    return join(__builtin_nontemporal_load(reinterpret_cast<const u4 *>(p)),
+                __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p + 64)));
+}
+
+// Sum of every wavefront's accumulators, in the order of the wavefronts; the
+// sum of piece i is returned to wavefront i % waves and visited with `then(i, sum)`.
+// lds: waves * PIECES KiB.
+template <int PIECES, class F>
+__device__ __forceinline__ void sum_waves(const f4 *acc, f4 *lds, int waves, int wave, int lane, F then) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        lds[(wave * PIECES + i) * 64 + lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < PIECES; i += waves) {
+        f4 sum = lds[i * 64 + lane];
+        for (int w = 1; w < waves; ++w)
+            sum += lds[(w * PIECES + i) * 64 + lane];
+        then(i, sum);
+    }
+}
+
+}  // namespace spconv

@@ -20,6 +20,7 @@
 #include "launch.hpp"
 #include "net_kernels.hpp"
 #include "planner.hpp"
+#include "status.hpp"
 
 struct spconv_plan_s {
     spconv::PackedPlan host;
@@ -528,6 +529,28 @@ spconv_status create_passes(spconv_plan_s *pl, const spconv::Input &in, const sp
 }
 
 }  // namespace
+
+namespace spconv {
+
+void clear_error() { g_err.clear(); }
+
+spconv_status set_error(spconv_status st, const char *msg) {
+    try {
+        g_err = msg;
+    } catch (const std::bad_alloc &) {
+    }
+    return st;
+}
+
+spconv_status set_hip_error(const char *what, hipError_t e) {
+    try {
+        return hip_fail(what, e);
+    } catch (const std::bad_alloc &) {
+        return SPCONV_E_HIP;
+    }
+}
+
+}  // namespace spconv
 
 extern "C" {
 

@@ -1,0 +1,133 @@
+"""Dense layers in 8 bits, for torch tensors.
+
+The arithmetic runs in libspconv's kernels (include/spconv.h says what each
+computes and how its arrays are laid out); this module checks shapes, types and
+strides, allocates what a call writes with torch's allocator (on the current
+stream, so that it is reused in order) and passes addresses on.
+
+Work is queued on ``stream`` (a torch stream; default: torch's current one).
+With another stream than the current one pass the outputs and the workspace
+too: torch may hand memory that it allocates here to the current stream's work
+before the other stream is done with it.
+"""
+
+from __future__ import annotations
+
+from .spconv import (BF16, F16, F32, FP8, spconv_linear_fp8, spconv_linear_fp8_workspace, spconv_quantize_fp8)
+
+BLOCK = 128
+_TYPES = {}
+
+
+def _type(t, what: str) -> int:
+    """The library's number for a tensor's element type."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError("%s must be float32, float16 or bfloat16, not %s" % (what, t.dtype)) from None
+
+
+def _matrix(x, what: str):
+    """(rows, cols, row stride) of a matrix on the GPU whose rows are contiguous."""
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError("%s must be a matrix on the GPU" % what)
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def _given(t, shape, dtype, device, what: str):
+    """t, checked to be a contiguous tensor of this shape and type on this device."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+    return t
+
+
+def _blocks(n: int) -> int:
+    return -(-n // BLOCK)
+
+
+def quantize_fp8(x, block_rows: int = 1, q=None, scale=None, stream=None):
+    """A matrix [rows, cols] as 8-bit codes [rows, 128 kb] (float8_e4m3fn, kb =
+    ceil(cols / 128)) and scales: [kb, rows] with block_rows = 1 (activations),
+    [ceil(rows / 128), kb] with block_rows = 128 (weights)."""
+    import torch
+    kind = _type(x, "x")
+    rows, cols, ld = _matrix(x, "x")
+    if block_rows not in (1, BLOCK):
+        raise ValueError("block_rows must be 1 or %d" % BLOCK)
+    kb = _blocks(cols)
+    shape, codes = (kb, rows) if block_rows == 1 else (_blocks(rows), kb), (rows, kb * BLOCK)
+    if q is None:
+        q = torch.empty(codes, dtype=torch.float8_e4m3fn, device=x.device)
+    else:
+        _given(q, codes, torch.float8_e4m3fn, x.device, "q")
+    if scale is None:
+        scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+    else:
+        _given(scale, shape, torch.float32, x.device, "scale")
+    if rows and cols:
+        spconv_quantize_fp8(x, kind, ld, rows, cols, block_rows, q, scale, stream)
+    return q, scale
+
+
+class Fp8Linear:
+    """A dense layer y = act(x W^T + b) with W [cout, cin] in 8 bits:
+    ``quantize_fp8(W, 128)``'s codes and scales.  It keeps the tensors given."""
+
+    def __init__(self, w, w_scale, cout: int, cin: int, bias=None, act: str = "none"):
+        import torch
+        if act not in ("none", "relu", "relu6"):
+            raise ValueError("act must be 'none', 'relu' or 'relu6'")
+        kb = _blocks(cin)
+        self.w = _given(w, (cout, kb * BLOCK), torch.float8_e4m3fn, w.device, "w")
+        self.w_scale = _given(w_scale, (_blocks(cout), kb), torch.float32, w.device, "w_scale")
+        self.bias = None if bias is None else _given(bias, (cout,), torch.float32, w.device, "bias")
+        self.cout, self.cin, self.act = int(cout), int(cin), act
+
+    @classmethod
+    def from_dense(cls, weight, bias=None, act: str = "none"):
+        """The layer of a weight [cout, cin] in float32, float16 or bfloat16."""
+        w, scale = quantize_fp8(weight, BLOCK)
+        return cls(w, scale, weight.shape[0], weight.shape[1], bias, act)
+
+    def workspace_bytes(self, n: int, dtype) -> int:
+        """Workspace of run() for n rows of a torch dtype that is not quantised yet."""
+        import torch
+        return spconv_linear_fp8_workspace(_type(torch.empty(0, dtype=dtype), "x"), n, self.cin, self.cout)
+
+    def run(self, x, x_scale=None, y=None, dtype=None, workspace=None, stream=None):
+        """y [n, cout] for x [n, cin], or for quantize_fp8's codes and scales
+        (then ``dtype`` or ``y`` gives y's type; it is x's otherwise)."""
+        import torch
+        dev = self.w.device
+        if x_scale is None:
+            kind = _type(x, "x")
+            n, cols, ld = _matrix(x, "x")
+            if cols != self.cin or x.device != dev:
+                raise ValueError("x must have %d channels and be on %s" % (self.cin, dev))
+            dtype = dtype or (x.dtype if y is None else y.dtype)
+        else:
+            n, kind, ld = int(x.shape[0]), FP8, 0
+            _given(x, (n, _blocks(self.cin) * BLOCK), torch.float8_e4m3fn, dev, "x")
+            _given(x_scale, (_blocks(self.cin), n), torch.float32, dev, "x_scale")
+            if dtype is None and y is None:
+                raise ValueError("quantised rows need y or its dtype")
+            dtype = dtype or y.dtype
+        if y is None:
+            y = torch.empty((n, self.cout), dtype=dtype, device=dev)
+        else:
+            _given(y, (n, self.cout), dtype, dev, "y")
+        size = spconv_linear_fp8_workspace(kind, n, self.cin, self.cout)
+        if size and workspace is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        elif size:
+            size = workspace.numel() * workspace.element_size()
+        if n:
+            spconv_linear_fp8(x, kind, ld, x_scale, self.w, self.w_scale, self.bias, self.act, y, _type(y, "y"), n,
+                              self.cin, self.cout, workspace if size else None, size, stream)
+        return y

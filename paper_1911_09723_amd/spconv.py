@@ -20,10 +20,12 @@ LIBRARY_PATH = os.path.join(_HERE, "libspconv.so")
 OK, E_ARG, E_FORMAT, E_SHAPE, E_UNSUPPORTED, E_NOMEM, E_HIP = range(7)
 STATUS_NAMES = {0: "SPCONV_OK", 1: "SPCONV_E_ARG", 2: "SPCONV_E_FORMAT", 3: "SPCONV_E_SHAPE",
                 4: "SPCONV_E_UNSUPPORTED", 5: "SPCONV_E_NOMEM", 6: "SPCONV_E_HIP"}
-F32, F16 = 0, 1
+F32, F16, BF16, FP8 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
 _ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "relu6": ACT_RELU6}
 _DTYPES = {"f32": F32, "f16": F16}
+# element types of the 8-bit products, the router and the experts
+_OP_DTYPES = {"f32": F32, "f16": F16, "bf16": BF16, "fp8": FP8}
 
 # Symbols declared in include/spconv.h.
 EXPORTED = ("spconv_plan_create", "spconv_run", "spconv_destroy", "spconv_last_error",
@@ -33,7 +35,8 @@ EXPORTED = ("spconv_plan_create", "spconv_run", "spconv_destroy", "spconv_last_e
             "spconv_global_avg_pool", "spconv_linear", "spconv_plan_create_blocked", "spconv_detect_blocks",
             "spconv_dense_to_bcsr_blocked", "spconv_plan_create_dense_blocked", "spconv_plan_unpack_indexed",
             "spconv_plan_check", "spconv_plan_set_wait_limit", "spconv_plan_create_static",
-            "spconv_plan_unpack_outer", "spconv_plan_run_kernel")
+            "spconv_plan_unpack_outer", "spconv_plan_run_kernel", "spconv_quantize_fp8", "spconv_linear_fp8",
+            "spconv_linear_fp8_workspace")
 
 
 class SpconvError(RuntimeError):
@@ -148,6 +151,13 @@ def load_library(path: Optional[str] = None):
     lib.spconv_linear.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp]
     lib.spconv_global_avg_pool.restype = i32
     lib.spconv_global_avg_pool.argtypes = [vp, vp, i32, i32, i32, i32, vp]
+    i64 = ctypes.c_int64
+    lib.spconv_quantize_fp8.restype = i32
+    lib.spconv_quantize_fp8.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp, vp]
+    lib.spconv_linear_fp8.restype = i32
+    lib.spconv_linear_fp8.argtypes = [vp, i32, i64, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, vp, i64, vp]
+    lib.spconv_linear_fp8_workspace.restype = i32
+    lib.spconv_linear_fp8_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
     if path is None:
         _lib = lib
     return lib
@@ -423,6 +433,40 @@ def spconv_global_avg_pool(x, y, n, c, h, w, stream=None, check: bool = True):
     if check:
         _check(status)
     return status
+
+
+def _op_dtype(dtype) -> int:
+    return _OP_DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+
+
+def spconv_quantize_fp8(x, dtype, ldx, rows, cols, block_rows, q, scale, stream=None, check: bool = True):
+    """Queue the conversion of a matrix to 8-bit codes and scales (device tensors or addresses)."""
+    status = load_library().spconv_quantize_fp8(_devptr(x), _op_dtype(dtype), int(ldx), int(rows), int(cols),
+                                                int(block_rows), _devptr(q), _devptr(scale), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_linear_fp8(x, x_dtype, ldx, x_scale, w, w_scale, bias, act, y, y_dtype, n, cin, cout, workspace=None,
+                      workspace_bytes=0, stream=None, check: bool = True):
+    """Queue the dense layer y = act(x W^T + b) with an 8-bit weight."""
+    a = _ACTS[act] if isinstance(act, str) else int(act)
+    status = load_library().spconv_linear_fp8(_devptr(x), _op_dtype(x_dtype), int(ldx), _devptr(x_scale), _devptr(w),
+                                              _devptr(w_scale), _devptr(bias), a, _devptr(y), _op_dtype(y_dtype),
+                                              int(n), int(cin), int(cout), _devptr(workspace), int(workspace_bytes),
+                                              _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_linear_fp8_workspace(x_dtype, n, cin, cout) -> int:
+    """Bytes of workspace that spconv_linear_fp8 needs."""
+    b = ctypes.c_int64()
+    _check(load_library().spconv_linear_fp8_workspace(_op_dtype(x_dtype), int(n), int(cin), int(cout),
+                                                      ctypes.byref(b)))
+    return b.value
 
 
 def spconv_destroy(plan):
