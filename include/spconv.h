@@ -343,6 +343,81 @@ SPCONV_API spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32
                                                      int64_t *bytes);
 
 /* ---------------------------------------------------------------------------
+ * Mixtures of experts: sparsity that is chosen for each token at run time.  A
+ * router picks k of many feed-forward networks for a token; only those run.
+ * Calls launch on `stream` as the 8-bit layers above do.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { SPCONV_SCORE_SOFTMAX = 0, SPCONV_SCORE_SIGMOID = 1 } spconv_score;
+
+/*
+ * Router: the experts of each token and their weights.  With l a token's logits,
+ *   s[e]     = exp(l[e]) / sum exp(l)  or  1 / (1 + exp(-l[e])),
+ *   value[e] = s[e] + bias[e]          (the bias balances the load: it changes
+ *                                       the choice, not the weights)
+ * An expert whose logit or value is -infinity or NaN is off: it takes no part
+ * (in the softmax's sum neither, for the logit); +infinity counts as the
+ * largest finite number.
+ * The experts form `groups` groups of neighbours; a group's rank is the sum of
+ * the group_top largest values in it (of those that are on), and experts
+ * outside the groups_kept best groups are not chosen.  Of the others the k
+ * largest values are chosen, in descending order; of equal values, and of
+ * equal groups, the lower index comes first.
+ *   weight = factor * s (with renorm != 0: factor * s / the sum of the chosen
+ *   s, or 0 where that sum is 0)
+ * Scores, values and sums are 64-bit, the weights are rounded once to fp32.
+ * Places that no expert is left for hold id -1 and weight 0.
+ *   logits  device, [n][experts] of dtype (F32, F16 or BF16), row stride ld >= experts elements
+ *   bias    device, [experts] floats, or NULL
+ *   ids     out, [n][k] int32_t      weights  out, [n][k] floats
+ * n == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, bad dtype, score or
+ * alignment, negative size, k < 1, groups < 1, groups_kept outside [1, groups],
+ * ld < experts, overlap), SPCONV_E_SHAPE (experts not a multiple of groups, k > experts, n of
+ * 2^25 or more), SPCONV_E_UNSUPPORTED (more than 1024 experts, 64 groups or
+ * k = 64, group_top not 1 or 2), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_route(const void *logits, spconv_dtype dtype, int64_t ld, const float *bias,
+                                      spconv_score score, int32_t n, int32_t experts, int32_t groups,
+                                      int32_t groups_kept, int32_t group_top, int32_t k, int32_t renorm, float factor,
+                                      int32_t *ids, float *weights, void *stream);
+
+/*
+ * The chosen experts' gated feed-forward networks, in 8 bits:
+ *   y[t] = sum_j weights[t][j] * W2[e] q( silu(W1[e] q(x[t])) * (W3[e] q(x[t])) ),  e = ids[t][j],
+ * with silu(v) = v / (1 + exp(-v)) and q the quantisation of a row as by
+ * spconv_quantize_fp8 with block_rows = 1.  An id outside [0, experts) has no
+ * term; a token with none gets zeros.  Products and sums are as for
+ * spconv_linear_fp8; the gate is applied in fp32, y is rounded once.
+ *   x        device, [n][hidden] of dtype (F32, F16 or BF16), row stride ldx >= hidden elements
+ *   ids, weights  device, [n][k], as spconv_route gives them (any order)
+ *   w13, w13_scale  W1 and W3 of each expert, [experts][2][inner][hidden] in
+ *            8-bit form, each matrix with its own 128 x 128 blocks:
+ *            scales [experts][2][ceil(inner / 128)][ceil(hidden / 128)]
+ *   w2, w2_scale    W2 likewise, [experts][hidden][inner], scales
+ *            [experts][ceil(hidden / 128)][ceil(inner / 128)]
+ *   y        device, [n][hidden] of dtype
+ *   workspace  device, 16-byte aligned, at least what
+ *            spconv_experts_fp8_workspace gives
+ * n == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, bad dtype or alignment,
+ * negative size, k < 1, ldx < hidden, workspace too small, overlap),
+ * SPCONV_E_SHAPE (experts, hidden or inner < 1, n * k * max(ceil(hidden / 128),
+ * ceil(inner / 128)) of 2^27 or more), SPCONV_E_UNSUPPORTED (more than 1024
+ * experts, k > 64, hidden or inner above 32768), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_experts_fp8(const void *x, spconv_dtype dtype, int64_t ldx, const int32_t *ids,
+                                            const float *weights, const void *w13, const float *w13_scale,
+                                            const void *w2, const float *w2_scale, void *y, int32_t n, int32_t k,
+                                            int32_t experts, int32_t hidden, int32_t inner, void *workspace,
+                                            int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace for such a call, host only.  Errors: SPCONV_E_ARG (NULL,
+ * negative size, k < 1), SPCONV_E_SHAPE and SPCONV_E_UNSUPPORTED as above. */
+SPCONV_API spconv_status spconv_experts_fp8_workspace(int32_t n, int32_t k, int32_t experts, int32_t hidden,
+                                                      int32_t inner, int64_t *bytes);
+
+/* ---------------------------------------------------------------------------
  * Planner controls and introspection.  These let a caller (and the CPU-only
  * tests) see what the host-side planner decided without running a kernel.
  * ------------------------------------------------------------------------- */

@@ -19,6 +19,8 @@ from .spconv import (  # noqa: F401
     spconv_global_avg_pool,
     spconv_detect_block_rows,
     spconv_detect_blocks,
+    spconv_experts_fp8,
+    spconv_experts_fp8_workspace,
     spconv_last_error,
     spconv_linear,
     spconv_linear_fp8,
@@ -41,9 +43,12 @@ from .spconv import (  # noqa: F401
     spconv_plan_set_wait_limit,
     SPCONV_FLAG_WAIT_GAVE_UP,
     spconv_quantize_fp8,
+    spconv_route,
     spconv_run,
 )
 from .experts import (  # noqa: F401
+    Experts,
     Fp8Linear,
     quantize_fp8,
+    route,
 )

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <limits>
+#include <type_traits>
 
 #include "expert_ops.hpp"
 #include "status.hpp"
@@ -86,6 +87,61 @@ int64_t linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t c
     if (x_dtype == SPCONV_FP8 || n == 0 || cout == 0 || spconv::linear_takes_rows(n, cin, cout))
         return 0;
     return code_bytes(n, cin) + align16(static_cast<int64_t>(n) * blocks_of(cin) * 4);
+}
+
+constexpr int32_t kMostExpertChannels = 32768;
+
+spconv_status check_experts(int32_t n, int32_t k, int32_t experts, int32_t hidden, int32_t inner) {
+    if (n < 0 || k < 1)
+        return set_error(SPCONV_E_ARG, "n must be >= 0 and k >= 1");
+    if (experts < 1 || hidden < 1 || inner < 1)
+        return set_error(SPCONV_E_SHAPE, "experts, hidden and inner must be >= 1");
+    if (experts > spconv::kMostExperts || k > spconv::kMostChoices)
+        return set_error(SPCONV_E_UNSUPPORTED, "at most 1024 experts and k = 64 are supported");
+    if (hidden > kMostExpertChannels || inner > kMostExpertChannels)
+        return set_error(SPCONV_E_UNSUPPORTED, "hidden and inner must be at most 32768");
+    if (static_cast<int64_t>(n) * k * blocks_of(hidden > inner ? hidden : inner) >= kMostBlocks)
+        return set_error(SPCONV_E_SHAPE, "n * k * ceil(channels / 128) must be below 2^27");
+    return SPCONV_OK;
+}
+
+// Lays the workspace of a call out from `base` (null: only counts) and returns its size.
+int64_t experts_layout(spconv::ExpertArgs &a, uint8_t *base) {
+    int64_t at = 0;
+    auto take = [&](auto &p, int64_t bytes) {
+        p = base ? reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at) : nullptr;
+        at += align16(bytes);
+    };
+    const int64_t pairs = a.pairs;
+    const spconv::ExpertPath path = spconv::expert_path(a.n, a.k, a.experts);
+    if (path != spconv::ExpertPath::kTokens) {
+        take(a.order, pairs * 4);
+        take(a.place, pairs * 4);
+        take(a.offsets, (a.experts + 1) * int64_t(4));
+        take(a.z, pairs * a.hidden * 4);
+    }
+    if (path == spconv::ExpertPath::kTiles) {
+        take(a.xq, code_bytes(a.n, a.hidden));
+        take(a.xs, static_cast<int64_t>(a.n) * a.hb * 4);
+        take(a.hq, code_bytes(pairs, a.inner));
+        take(a.hs, pairs * a.ib * 4);
+    } else {
+        take(a.h, pairs * a.inner * 4);
+    }
+    return at;
+}
+
+spconv::ExpertArgs expert_sizes(int32_t n, int32_t k, int32_t experts, int32_t hidden, int32_t inner) {
+    spconv::ExpertArgs a{};
+    a.n = n;
+    a.k = k;
+    a.pairs = n * k;
+    a.experts = experts;
+    a.hidden = hidden;
+    a.inner = inner;
+    a.hb = blocks_of(hidden);
+    a.ib = blocks_of(inner);
+    return a;
 }
 
 }  // namespace
@@ -197,6 +253,119 @@ spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx
         a.x_type = spconv::kFp8;
     }
     return launched(spconv::launch_linear_fp8(a, s));
+}
+
+spconv_status spconv_route(const void *logits, spconv_dtype dtype, int64_t ld, const float *bias, spconv_score score,
+                           int32_t n, int32_t experts, int32_t groups, int32_t groups_kept, int32_t group_top,
+                           int32_t k, int32_t renorm, float factor, int32_t *ids, float *weights, void *stream) {
+    spconv::clear_error();
+    if (!is_float(dtype))
+        return set_error(SPCONV_E_ARG, "dtype must be SPCONV_F32, _F16 or _BF16");
+    if (score != SPCONV_SCORE_SOFTMAX && score != SPCONV_SCORE_SIGMOID)
+        return set_error(SPCONV_E_ARG, "score must be SPCONV_SCORE_SOFTMAX or _SIGMOID");
+    if (n < 0 || experts < 1 || k < 1)
+        return set_error(SPCONV_E_ARG, "n must be >= 0, experts and k >= 1");
+    if (groups < 1 || groups_kept < 1 || groups_kept > groups)
+        return set_error(SPCONV_E_ARG, "groups must be >= 1 and groups_kept in [1, groups]");
+    if (experts % groups != 0 || k > experts)
+        return set_error(SPCONV_E_SHAPE, "experts must be a multiple of groups and k at most experts");
+    if (experts > spconv::kMostExperts || groups > 64 || k > spconv::kMostChoices || group_top < 1 || group_top > 2)
+        return set_error(SPCONV_E_UNSUPPORTED, "at most 1024 experts, 64 groups and k = 64, and group_top 1 or 2");
+    if (n >= 1 << 25)
+        return set_error(SPCONV_E_SHAPE, "n must be below 2^25");
+    if (n == 0)
+        return SPCONV_OK;
+    if (!logits || !ids || !weights)
+        return set_error(SPCONV_E_ARG, "logits, ids or weights is NULL");
+    if (ld < experts)
+        return set_error(SPCONV_E_ARG, "ld must be at least experts");
+    if (ld > kMostStride)
+        return set_error(SPCONV_E_SHAPE, "ld must be at most 2^34");
+    if (!aligned(logits, size_of(dtype)) || !aligned(bias, 4) || !aligned(ids, 4) || !aligned(weights, 4))
+        return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size");
+    const int64_t places = static_cast<int64_t>(n) * k * 4;
+    const Range in[] = {{logits, span(n, experts, ld, size_of(dtype))}, {bias, experts * int64_t(4)}};
+    const Range out[] = {{ids, places}, {weights, places}};
+    if (outputs_overlap(out, in))
+        return set_error(SPCONV_E_ARG, "ids and weights must not overlap each other or an input");
+    spconv::RouteArgs a{};
+    a.logits = logits;
+    a.ld = ld;
+    a.bias = bias;
+    a.ids = ids;
+    a.weights = weights;
+    a.n = n;
+    a.experts = experts;
+    a.k = k;
+    a.groups = groups;
+    a.groups_kept = groups_kept;
+    a.group_top = group_top;
+    a.softmax = score == SPCONV_SCORE_SOFTMAX;
+    a.renorm = renorm != 0;
+    a.factor = factor;
+    return launched(spconv::launch_route(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+spconv_status spconv_experts_fp8_workspace(int32_t n, int32_t k, int32_t experts, int32_t hidden, int32_t inner,
+                                           int64_t *bytes) {
+    spconv::clear_error();
+    if (!bytes)
+        return set_error(SPCONV_E_ARG, "bytes is NULL");
+    *bytes = 0;
+    const spconv_status st = check_experts(n, k, experts, hidden, inner);
+    if (st != SPCONV_OK || n == 0)
+        return st;
+    spconv::ExpertArgs a = expert_sizes(n, k, experts, hidden, inner);
+    *bytes = experts_layout(a, nullptr);
+    return SPCONV_OK;
+}
+
+spconv_status spconv_experts_fp8(const void *x, spconv_dtype dtype, int64_t ldx, const int32_t *ids,
+                                 const float *weights, const void *w13, const float *w13_scale, const void *w2,
+                                 const float *w2_scale, void *y, int32_t n, int32_t k, int32_t experts, int32_t hidden,
+                                 int32_t inner, void *workspace, int64_t workspace_bytes, void *stream) {
+    spconv::clear_error();
+    if (!is_float(dtype))
+        return set_error(SPCONV_E_ARG, "dtype must be SPCONV_F32, _F16 or _BF16");
+    const spconv_status st = check_experts(n, k, experts, hidden, inner);
+    if (st != SPCONV_OK || n == 0)
+        return st;
+    if (!x || !ids || !weights || !w13 || !w13_scale || !w2 || !w2_scale || !y || !workspace)
+        return set_error(SPCONV_E_ARG, "a pointer is NULL");
+    if (ldx < hidden)
+        return set_error(SPCONV_E_ARG, "ldx must be at least hidden");
+    if (ldx > kMostStride)
+        return set_error(SPCONV_E_SHAPE, "ldx must be at most 2^34");
+    const int64_t size = size_of(dtype);
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(w13, 16) ||
+        !aligned(w13_scale, 4) || !aligned(w2, 16) || !aligned(w2_scale, 4) || !aligned(workspace, 16))
+        return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size, codes and the workspace to 16 bytes");
+    spconv::ExpertArgs a = expert_sizes(n, k, experts, hidden, inner);
+    const int64_t need = experts_layout(a, static_cast<uint8_t *>(workspace));
+    if (workspace_bytes < need)
+        return set_error(SPCONV_E_ARG, "the workspace is smaller than spconv_experts_fp8_workspace says");
+    const int64_t scales = static_cast<int64_t>(experts) * a.hb * a.ib * 4;
+    const Range in[] = {{x, span(n, hidden, ldx, size)},
+                        {ids, a.pairs * int64_t(4)},
+                        {weights, a.pairs * int64_t(4)},
+                        {w13, experts * 2 * code_bytes(inner, hidden)},
+                        {w13_scale, 2 * scales},
+                        {w2, experts * code_bytes(hidden, inner)},
+                        {w2_scale, scales}};
+    const Range out[] = {{y, static_cast<int64_t>(n) * hidden * size}, {workspace, need}};
+    if (outputs_overlap(out, in))
+        return set_error(SPCONV_E_ARG, "y and the workspace must not overlap each other or an input");
+    a.x = x;
+    a.ldx = ldx;
+    a.type = dtype;
+    a.ids = ids;
+    a.weights = weights;
+    a.w13 = static_cast<const uint8_t *>(w13);
+    a.s13 = w13_scale;
+    a.w2 = static_cast<const uint8_t *>(w2);
+    a.s2 = w2_scale;
+    a.y = y;
+    return launched(spconv::launch_experts(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -39,4 +39,54 @@ struct LinearArgs {
 bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout);
 hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream);
 
+// Router: ids and weights [n][k] from logits [n][experts] (row stride ld elements).
+struct RouteArgs {
+    const void *logits;
+    int64_t ld;
+    const float *bias;  // [experts] or null
+    int32_t *ids;
+    float *weights;
+    int32_t n, experts, k;
+    int32_t groups, groups_kept, group_top;
+    int32_t softmax, renorm;
+    float factor;
+    // set by launch_route: experts of a group and its inverse, lanes that look through one
+    int32_t each;
+    uint32_t each_inverse;
+    int32_t group_lanes;
+};
+constexpr int32_t kMostExperts = 1024;
+constexpr int32_t kMostChoices = 64;
+hipError_t launch_route(RouteArgs a, int32_t type, hipStream_t stream);
+
+// Pairs (token, choice) sorted by expert, stable: order[place] = pair, place[pair]
+// (-1: its id is no expert), offsets[experts + 1] = each expert's first place.
+hipError_t launch_sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order, int32_t *place,
+                             int32_t *offsets, hipStream_t stream);
+
+// The experts' networks over pairs (token, choice), pairs = n k.
+struct ExpertArgs {
+    const void *x;             // [n][hidden], row stride ldx elements
+    int64_t ldx;
+    const int32_t *ids;        // [n][k]
+    const float *weights;      // [n][k]
+    const uint8_t *w13, *w2;   // codes [experts][2][inner][128 hb], [experts][hidden][128 ib]
+    const float *s13, *s2;     // scales [experts][2][ib][hb], [experts][hb][ib]
+    void *y;                   // [n][hidden]
+    int32_t type;              // of x and y
+    int32_t n, k, pairs, experts, hidden, inner;
+    int32_t hb, ib;            // blocks of 128 hidden and inner channels
+    // workspace: the pairs' order by expert, x's codes, the inner rows by place
+    // (in 32 bits or as codes), the results by place
+    int32_t *order, *place, *offsets;
+    uint8_t *xq, *hq;
+    float *xs, *hs, *h, *z;
+};
+
+// How a call is run: token by token (each pair reads its expert's weights), by
+// expert with the rows of 16 at a time against streamed weights, or over LDS tiles.
+enum class ExpertPath { kTokens, kFew, kTiles };
+ExpertPath expert_path(int32_t n, int32_t k, int32_t experts);
+hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream);
+
 }  // namespace spconv

@@ -1,0 +1,485 @@
+// The gated feed-forward networks of the experts that a router chose:
+//
+//   y[t] = sum_j weight[t][j] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = ids[t][j]
+//
+// in 8 bits with block scales (fp8.hpp; q quantises by row).  A pair (token,
+// choice) is one row of work.
+#include <algorithm>
+
+#include "expert_ops.hpp"
+#include "fp8_product.hpp"
+
+namespace spconv {
+namespace {
+
+constexpr int kXcds = 8;
+
+// g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each;
+// g log2(e) is taken to twice 32 bits so that the exponential stays there.
+__device__ __forceinline__ float gated(float g, float u) {
+    const float t = g * -1.44269504f, rest = fmaf(g, -1.44269504f, -t) + g * -1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    const float exact = fabsf(t) < 128.0f ? fmaf(e, rest * 0.693147181f, e) : e;  // else 0 or infinite
+    return g * __builtin_amdgcn_rcpf(1.0f + exact) * u;
+}
+
+// One tile of rows of one expert, places [row, row + rows).
+struct RowTile {
+    int32_t expert, row, rows;
+};
+
+// Tile `id` of all (tile of `high` rows, column tile of `wide`), in the order
+// that gives each XCD one run of neighbouring tiles: tiles of one expert share
+// its weights, and column tiles the rows, in an L2.  False past the last one.
+// Every lane takes 64th expert; the scans are over a wavefront.
+__device__ __forceinline__ bool find_tile(const int32_t *offsets, int32_t experts, int32_t high, int32_t wide,
+                                          int lane, RowTile *tile, int32_t *column) {
+    auto tiles_of = [&](int32_t e) {
+        return e < experts ? (offsets[e + 1] - offsets[e] + high - 1) / high : 0;
+    };
+    int32_t total = 0;
+    for (int32_t e0 = 0; e0 < experts; e0 += 64)
+        total += tiles_of(e0 + lane);
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+        total += __shfl_xor(total, s);
+    const int32_t per = (total * wide + kXcds - 1) / kXcds;
+    const int32_t in = blockIdx.x / kXcds, id = blockIdx.x % kXcds * per + in;
+    if (in >= per || id >= total * wide)
+        return false;
+    int32_t want = id / wide;
+    *column = id - want * wide;
+    for (int32_t e0 = 0; e0 < experts; e0 += 64) {
+        const int32_t own = tiles_of(e0 + lane);
+        int32_t upto = own;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const int32_t o = __shfl_up(upto, s);
+            upto += lane >= s ? o : 0;
+        }
+        const uint64_t past = __ballot(upto > want);
+        if (past) {
+            const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
+            const int32_t before = __shfl(upto - own, at);
+            tile->expert = __builtin_amdgcn_readfirstlane(e0 + at);
+            const int32_t row = offsets[tile->expert] + (want - before) * high;
+            tile->row = __builtin_amdgcn_readfirstlane(row);
+            tile->rows = __builtin_amdgcn_readfirstlane(min(high, offsets[tile->expert + 1] - row));
+            *column = __builtin_amdgcn_readfirstlane(*column);
+            return true;
+        }
+        want -= __shfl(upto, 63);
+    }
+    return false;
+}
+
+// First products over LDS tiles: 128 inner channels, gate and up, of a tile of
+// rows, which are x's rows (codes) by token; the result leaves as codes.  A
+// wavefront holds 64 gate and the same 64 up channels, so that the gate is
+// applied in its registers; the block's largest magnitude is joined over the
+// two wavefronts that share its rows.
+template <class S, bool EXACT>
+__global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t columns) {
+    static_assert(S::BC == 256 && S::WC == 2, "a wavefront holds half a block of gate and of up channels");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    RowTile tile;
+    int32_t fb;
+    if (!find_tile(a.offsets, a.experts, S::BT, columns, lane, &tile, &fb))
+        return;
+    const int64_t pitch = static_cast<int64_t>(a.hb) * kBlock;
+    const uint8_t *w = a.w13 + static_cast<int64_t>(tile.expert) * 2 * a.inner * pitch;
+    const float *ws = a.s13 + static_cast<int64_t>(tile.expert) * 2 * a.ib * a.hb + static_cast<int64_t>(fb) * a.hb;
+    const uint8_t *src[S::kLoads];
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const int line = tile_line<S>(wave, lane, i);
+        const uint8_t *row;
+        if (line < S::BC) {  // lines of a wavefront: 64 gate, then 64 up channels
+            const int32_t ch = min(fb * kBlock + line / 128 * 64 + line % 64, a.inner - 1);
+            row = w + (ch + (line & 64 ? a.inner : 0)) * pitch;
+        } else {
+            const int32_t pair = a.order[tile.row + min(line - S::BC, tile.rows - 1)];
+            row = a.xq + (pair / a.k) * pitch;
+        }
+        src[i] = row + tile_byte(line, lane);
+    }
+    const float *xs = a.xs;
+    if (wave < S::BT / 64)
+        xs += a.order[tile.row + min(wave * 64 + lane, tile.rows - 1)] / a.k;
+    f4 acc[S::NC][S::NT] = {};
+    tile_product<S, EXACT, true>(acc, src, xs, a.n, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
+
+    const int wc = wave / S::WT, wt = wave % S::WT;
+    float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
+    constexpr int HC = S::NC / 2;
+    uint32_t m[S::NT];
+#pragma unroll
+    for (int t = 0; t < S::NT; ++t) {
+        m[t] = 0;
+#pragma unroll
+        for (int c = 0; c < HC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t ch = fb * kBlock + wc * 64 + c * 16 + (lane >> 4) * 4 + i;
+                const float h = ch < a.inner ? gated(acc[c][t][i], acc[c + HC][t][i]) : 0.0f;
+                acc[c][t][i] = h;
+                m[t] = max(m[t], magnitude(h));
+            }
+        m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 16)));
+        m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 32)));
+        if (lane < 16)
+            most[wc * S::BT + (wt * S::NT + t) * 16 + lane] = __uint_as_float(m[t]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < S::NT; ++t) {
+        const int r = (wt * S::NT + t) * 16 + (lane & 15);
+        const Scale s = scale_of(max(m[t], __float_as_uint(most[(1 - wc) * S::BT + r])));
+#pragma unroll
+        for (int c = 0; c < HC; ++c) {
+            const float v[4] = {acc[c][t][0], acc[c][t][1], acc[c][t][2], acc[c][t][3]};
+            const int word = (wc * 16 + c * 4 + (lane >> 4)) ^ (r & 7) * 4;  // spread over LDS's banks
+            reinterpret_cast<uint32_t *>(lds)[r * 32 + word] = codes4(v, s.inv);
+        }
+        if (wc == 0 && lane < 16 && r < tile.rows)
+            a.hs[static_cast<int64_t>(fb) * a.pairs + tile.row + r] = s.scale;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BT * 8; i += S::kThreads) {
+        const int r = i >> 3, piece = i & 7;
+        if (r < tile.rows)
+            *reinterpret_cast<u4 *>(a.hq + (static_cast<int64_t>(tile.row + r) * a.ib + fb) * kBlock + piece * 16) =
+                *reinterpret_cast<const u4 *>(lds + r * kBlock + ((piece ^ (r & 7)) * 16));
+    }
+}
+
+// Second products over LDS tiles: rows by place, results by place in 32 bits.
+template <class S, bool EXACT>
+__global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t columns) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    RowTile tile;
+    int32_t ct;
+    if (!find_tile(a.offsets, a.experts, S::BT, columns, lane, &tile, &ct))
+        return;
+    const int32_t c0 = ct * S::BC;
+    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
+    const uint8_t *w = a.w2 + static_cast<int64_t>(tile.expert) * a.hidden * pitch;
+    const uint8_t *src[S::kLoads];
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const int line = tile_line<S>(wave, lane, i);
+        const uint8_t *row = line < S::BC ? w + min(c0 + line, a.hidden - 1) * pitch
+                                          : a.hq + (tile.row + min(line - S::BC, tile.rows - 1)) * pitch;
+        src[i] = row + tile_byte(line, lane);
+    }
+    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int32_t cw = c0 + wc * S::NC * 16;
+    const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + min(cw, a.hidden - 1) / kBlock) * a.ib;
+    const float *xs = a.hs + tile.row + min(wave * 64 + lane, tile.rows - 1);
+    f4 acc[S::NC][S::NT] = {};
+    tile_product<S, EXACT, false>(acc, src, xs, a.pairs, ws, nullptr, a.ib, lds, wave, lane);
+#pragma unroll
+    for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+        for (int t = 0; t < S::NT; ++t) {
+            const int r = (wt * S::NT + t) * 16 + (lane & 15);
+            const int32_t ch = cw + c * 16 + (lane >> 4) * 4;
+            if (r < tile.rows && ch < a.hidden)
+                store4(a.z, kF32, static_cast<int64_t>(tile.row + r) * a.hidden + ch, acc[c][t], a.hidden - ch,
+                       a.hidden % 4 == 0);
+        }
+}
+
+// First products of a few rows: 16 gate and 16 up channels of up to 16 rows, which are
+// quantised here.  DIRECT: a workgroup's row is pair blockIdx.y itself, unsorted.
+template <typename T, int U, bool DIRECT>
+__global__ void __launch_bounds__(1024) gated_stream(ExpertArgs a, int32_t columns, bool wide) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    RowTile tile;
+    int32_t ct;
+    int32_t token;
+    if constexpr (DIRECT) {
+        tile = RowTile{a.ids[blockIdx.y], static_cast<int32_t>(blockIdx.y), 1};
+        ct = blockIdx.x;
+        if (tile.expert < 0 || tile.expert >= a.experts)
+            return;
+        token = tile.row / a.k;
+    } else {
+        if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &ct))
+            return;
+        token = a.order[tile.row + min(lane & 15, tile.rows - 1)] / a.k;
+    }
+    const int32_t c0 = ct * 16;
+    const int64_t pitch = static_cast<int64_t>(a.hb) * kBlock;
+    const uint8_t *wg = a.w13 + (static_cast<int64_t>(tile.expert) * 2 * a.inner + min(c0 + (lane & 15), a.inner - 1)) * pitch;
+    const uint8_t *wu = wg + a.inner * pitch;
+    const float *sg = a.s13 + (static_cast<int64_t>(tile.expert) * 2 * a.ib + c0 / kBlock) * a.hb;
+    const float *su = sg + static_cast<int64_t>(a.ib) * a.hb;
+    const T *x = static_cast<const T *>(a.x) + token * a.ldx;
+    f4 acc[2] = {};
+    for (int32_t b0 = wave; b0 < a.hb; b0 += waves * U) {
+        i8 g[U], up[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.hb - 1);
+            g[u] = weight_part(wg, b, lane);
+            up[u] = weight_part(wu, b, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = b0 + u * waves;
+            if (b >= a.hb)
+                break;
+            const RowPart xp = row_quantized(x, b, a.hidden, wide, lane);
+            const Halves xh = halves(xp.code);
+            const f4 p = mfma128(halves(g[u]), xh), q = mfma128(halves(up[u]), xh);
+            const float s0 = xp.scale * sg[b], s1 = xp.scale * su[b];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                acc[0][i] = fmaf(s0, p[i], acc[0][i]);
+                acc[1][i] = fmaf(s1, q[i], acc[1][i]);
+            }
+        }
+    }
+    f4 *all = reinterpret_cast<f4 *>(lds);
+    all[(wave * 2) * 64 + lane] = acc[0];
+    all[(wave * 2 + 1) * 64 + lane] = acc[1];
+    __syncthreads();
+    if (wave > 0)
+        return;
+    f4 gate = all[lane], up = all[64 + lane];
+    for (int w = 1; w < waves; ++w) {
+        gate += all[w * 128 + lane];
+        up += all[w * 128 + 64 + lane];
+    }
+    const int32_t ch = c0 + (lane >> 4) * 4;
+    if ((lane & 15) < tile.rows && ch < a.inner) {
+        f4 h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            h[i] = gated(gate[i], up[i]);
+        store4(a.h, kF32, static_cast<int64_t>(tile.row + (lane & 15)) * a.inner + ch, h, a.inner - ch, a.inner % 4 == 0);
+    }
+}
+
+// Second products of a few rows, quantised here; results by place in 32 bits.
+template <int CT, int U>
+__global__ void __launch_bounds__(1024) down_stream(ExpertArgs a, int32_t columns) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    RowTile tile;
+    int32_t ct;
+    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &ct))
+        return;
+    const int32_t c0 = ct * 16 * CT;
+    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
+    const uint8_t *w[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+        w[c] = a.w2 + (static_cast<int64_t>(tile.expert) * a.hidden + min(c0 + c * 16 + (lane & 15), a.hidden - 1)) * pitch;
+    const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + c0 / kBlock) * a.ib;
+    const float *h = a.h + static_cast<int64_t>(tile.row + min(lane & 15, tile.rows - 1)) * a.inner;
+    f4 acc[CT] = {};
+    for (int32_t b0 = wave; b0 < a.ib; b0 += waves * U) {
+        i8 wf[U][CT];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                wf[u][c] = weight_part(w[c], min(b0 + u * waves, a.ib - 1), lane);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = b0 + u * waves;
+            if (b >= a.ib)
+                break;
+            const RowPart xp = row_quantized(h, b, a.inner, a.inner % 4 == 0, lane);
+            const Halves xh = halves(xp.code);
+            const float s = xp.scale * ws[b];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const f4 p = mfma128(halves(wf[u][c]), xh);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[c][i] = fmaf(s, p[i], acc[c][i]);
+            }
+        }
+    }
+    sum_waves<CT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int c, f4 sum) {
+        const int32_t ch = c0 + c * 16 + (lane >> 4) * 4;
+        if ((lane & 15) < tile.rows && ch < a.hidden)
+            store4(a.z, kF32, static_cast<int64_t>(tile.row + (lane & 15)) * a.hidden + ch, sum, a.hidden - ch,
+                   a.hidden % 4 == 0);
+    });
+}
+
+// Second products and weighted sum of one token (blockIdx.y): the pairs' blocks
+// of inner channels are one long axis, dealt to the wavefronts in turn.
+__global__ void __launch_bounds__(1024) down_token(ExpertArgs a, bool wide) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int32_t c0 = blockIdx.x * 16, token = blockIdx.y;
+    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
+    f4 acc[1] = {};
+    for (int32_t item = wave; item < a.k * a.ib; item += waves) {
+        const int32_t j = item / a.ib, b = item - j * a.ib, pair = token * a.k + j;
+        const int32_t e = a.ids[pair];
+        if (e < 0 || e >= a.experts)
+            continue;
+        const int64_t row = static_cast<int64_t>(e) * a.hidden + min(c0 + (lane & 15), a.hidden - 1);
+        const i8 wf = weight_part(a.w2 + row * pitch, b, lane);
+        const RowPart xp = row_quantized(a.h + static_cast<int64_t>(pair) * a.inner, b, a.inner, a.inner % 4 == 0, lane);
+        const f4 p = mfma128(halves(wf), halves(xp.code));
+        const float s = xp.scale * a.s2[(static_cast<int64_t>(e) * a.hb + c0 / kBlock) * a.ib + b] * a.weights[pair];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            acc[0][i] = fmaf(s, p[i], acc[0][i]);
+    }
+    sum_waves<1>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int, f4 sum) {
+        const int32_t ch = c0 + (lane >> 4) * 4;
+        if ((lane & 15) == 0 && ch < a.hidden)
+            store4(a.y, a.type, static_cast<int64_t>(token) * a.hidden + ch, sum, a.hidden - ch, wide);
+    });
+}
+
+// y[t] = sum_j weights[t][j] * z[place of (t, j)], in 32 bits, in the order of j.
+__global__ void __launch_bounds__(256) combine(ExpertArgs a, int32_t pieces, bool wide) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int32_t token = static_cast<int32_t>(id / pieces), ch = static_cast<int32_t>(id % pieces) * 4;
+    if (token >= a.n)
+        return;
+    f4 sum = {0, 0, 0, 0};
+    for (int32_t j = 0; j < a.k; ++j) {
+        const int32_t pair = token * a.k + j, at = a.place[pair];
+        if (at < 0)
+            continue;
+        const float w = a.weights[pair];
+        const float *z = a.z + static_cast<int64_t>(at) * a.hidden + ch;
+        if (a.hidden % 4 == 0) {
+            const f4 v = *reinterpret_cast<const f4 *>(z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sum[i] = fmaf(w, v[i], sum[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (ch + i < a.hidden)
+                    sum[i] = fmaf(w, z[i], sum[i]);
+        }
+    }
+    store4(a.y, a.type, static_cast<int64_t>(token) * a.hidden + ch, sum, a.hidden - ch, wide);
+}
+
+template <typename F>
+hipError_t allow_lds(F *kernel, int bytes) {
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+// Most tiles of `high` rows that pairs of so many experts can make.
+int64_t most_tiles(const ExpertArgs &a, int32_t high) {
+    return std::min<int64_t>(a.pairs, a.pairs / high + std::min(a.experts, a.pairs));
+}
+
+uint32_t tile_grid(int64_t tiles, int64_t columns) {
+    return static_cast<uint32_t>((tiles * columns + kXcds - 1) / kXcds * kXcds);
+}
+
+template <class S, bool EXACT>
+hipError_t gated_tiles(const ExpertArgs &a, hipStream_t stream) {
+    static const hipError_t ready = allow_lds(gated_tile<S, EXACT>, S::kLds);
+    if (ready != hipSuccess)
+        return ready;
+    gated_tile<S, EXACT><<<tile_grid(most_tiles(a, S::BT), a.ib), S::kThreads, S::kLds, stream>>>(a, a.ib);
+    return hipGetLastError();
+}
+
+template <class S, bool EXACT>
+hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
+    static const hipError_t ready = allow_lds(down_tile<S, EXACT>, S::kLds);
+    if (ready != hipSuccess)
+        return ready;
+    const int32_t columns = (a.hidden + S::BC - 1) / S::BC;
+    down_tile<S, EXACT><<<tile_grid(most_tiles(a, S::BT), columns), S::kThreads, S::kLds, stream>>>(a, columns);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t gated_few(const ExpertArgs &a, bool direct, hipStream_t stream) {
+    const int32_t columns = (a.inner + 15) / 16;
+    const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
+    const int waves = std::min(a.hb, 8);
+    const size_t lds = static_cast<size_t>(waves) * 2048;
+    if (direct)
+        gated_stream<T, 2, true><<<dim3(columns, a.pairs), waves * 64, lds, stream>>>(a, columns, wide);
+    else
+        gated_stream<T, 2, false><<<tile_grid(most_tiles(a, 16), columns), waves * 64, lds, stream>>>(a, columns, wide);
+    return hipGetLastError();
+}
+
+hipError_t gated_few(const ExpertArgs &a, bool direct, hipStream_t stream) {
+    return a.type == kF32 ? gated_few<float>(a, direct, stream)
+           : a.type == kF16 ? gated_few<_Float16>(a, direct, stream)
+                            : gated_few<__bf16>(a, direct, stream);
+}
+
+}  // namespace
+
+ExpertPath expert_path(int32_t n, int32_t k, int32_t experts) {
+    const int64_t pairs = static_cast<int64_t>(n) * k;
+    if (n <= 4 && pairs <= 64)
+        return ExpertPath::kTokens;
+    return pairs <= 16ll * experts ? ExpertPath::kFew : ExpertPath::kTiles;
+}
+
+hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
+    const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
+    const ExpertPath path = expert_path(a.n, a.k, a.experts);
+    hipError_t e;
+    if (path == ExpertPath::kTokens) {
+        if ((e = gated_few(a, true, stream)) != hipSuccess)
+            return e;
+        const int waves = std::min(a.k * a.ib, 16);
+        down_token<<<dim3((a.hidden + 15) / 16, a.n), waves * 64, waves * 1024, stream>>>(a, wide);
+        return hipGetLastError();
+    }
+    if ((e = launch_sort_pairs(a.ids, a.pairs, a.experts, a.order, a.place, a.offsets, stream)) != hipSuccess)
+        return e;
+    if (path == ExpertPath::kFew) {
+        if ((e = gated_few(a, false, stream)) != hipSuccess)
+            return e;
+        const int32_t columns = (a.hidden + 31) / 32;
+        const int waves = std::min(a.ib, 8);
+        down_stream<2, 1><<<tile_grid(most_tiles(a, 16), columns), waves * 64, waves * 2048, stream>>>(a, columns);
+        e = hipGetLastError();
+    } else {
+        using Small = TileShape<256, 64, 2, 4>;
+        using Mid = TileShape<256, 128, 2, 4>;
+        const bool high = a.pairs > 96ll * a.experts;
+        if ((e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
+            return e;
+        // bf16: what the 8-bit instruction loses lies below the rounding of the result
+        if (a.type == kBf16)
+            e = high ? gated_tiles<Mid, false>(a, stream) : gated_tiles<Small, false>(a, stream);
+        else
+            e = gated_tiles<Small, true>(a, stream);
+        if (e != hipSuccess)
+            return e;
+        if (a.type == kF32)
+            e = down_tiles<TileShape<128, 128, 2, 2>, true>(a, stream);
+        else
+            e = high ? down_tiles<Mid, false>(a, stream) : down_tiles<Small, false>(a, stream);
+    }
+    if (e != hipSuccess)
+        return e;
+    const int32_t pieces = (a.hidden + 3) / 4;
+    const int64_t blocks = (static_cast<int64_t>(a.n) * pieces + 255) / 256;
+    combine<<<static_cast<uint32_t>(blocks), 256, 0, stream>>>(a, pieces, wide);
+    return hipGetLastError();
+}
+
+}  // namespace spconv

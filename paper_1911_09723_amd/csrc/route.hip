@@ -1,0 +1,284 @@
+// The experts of each token, and the order of the rows that they work on.
+//
+// Routing: s = softmax(l) or 1 / (1 + exp(-l)) over a token's logits, value =
+// s + bias; experts in equal groups, a group's rank is the sum of its one or
+// two largest values; the best k values of the best groups, ties to the lowest
+// index, and the chosen s, divided by their sum where asked, times a factor.
+// Scores and values are 64-bit: neither the rounding of exp nor the order of
+// the softmax's sum then decides between two experts that are nearly tied, so
+// that every program that follows the definition chooses the same ones.
+#include <algorithm>
+
+#include "expert_ops.hpp"
+#include "fp8.hpp"
+
+namespace spconv {
+namespace {
+
+// A 64-bit value as a whole number of the same order; 0 is below every value.
+__device__ __forceinline__ uint64_t key_of(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return b >> 63 ? ~b : b | uint64_t(1) << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t key) {
+    return __builtin_bit_cast(double, key >> 63 ? key & ~(uint64_t(1) << 63) : ~key);
+}
+
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+#define SPCONV_STEP(ctrl, rows) \
+    v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), ctrl, rows, 0xf, false)))
+    SPCONV_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8
+    SPCONV_STEP(0x112, 0xf);
+    SPCONV_STEP(0x114, 0xf);
+    SPCONV_STEP(0x118, 0xf);
+    SPCONV_STEP(0x142, 0xa);  // row_bcast:15, 31
+    SPCONV_STEP(0x143, 0xc);
+#undef SPCONV_STEP
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+
+// The wavefront's largest key, and the lanes that hold it.
+__device__ __forceinline__ uint64_t key_max(uint64_t key, uint64_t *lanes) {
+    const uint32_t hi = dpp_max(static_cast<uint32_t>(key >> 32));
+    const bool same = static_cast<uint32_t>(key >> 32) == hi;
+    const uint32_t lo = dpp_max(same ? static_cast<uint32_t>(key) : 0);
+    *lanes = __ballot(same && static_cast<uint32_t>(key) == lo);
+    return static_cast<uint64_t>(hi) << 32 | lo;
+}
+
+__device__ __forceinline__ double sum_lanes(double v) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+        v += __shfl_xor(v, s);
+    return v;
+}
+
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(b), lane);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane);
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// A wavefront a token; a lane holds PER neighbouring experts, so that the
+// lowest lane of a tie holds the lowest expert.
+template <typename T, int PER>
+__global__ void __launch_bounds__(256) route_kernel(RouteArgs a, bool wide) {
+    extern __shared__ __attribute__((aligned(16))) uint64_t lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t token = blockIdx.x * 4 + wave;
+    const int32_t e0 = lane * PER;
+    if (token >= a.n)
+        return;
+    const T *l = static_cast<const T *>(a.logits) + token * a.ld + e0;
+    float v[PER];
+    if (wide && e0 + PER <= a.experts) {
+        struct __attribute__((aligned(sizeof(T) * PER > 16 ? 16 : sizeof(T) * PER))) Piece {
+            T v[PER];
+        } p = *reinterpret_cast<const Piece *>(l);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            v[i] = static_cast<float>(p.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            v[i] = e0 + i < a.experts ? static_cast<float>(l[i]) : -INFINITY;
+    }
+    double score[PER];
+    uint64_t key[PER];
+    if (a.softmax) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            v[i] = fminf(v[i] != v[i] ? -INFINITY : v[i], 3.402823466e38f);
+            most = fmaxf(most, v[i]);
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2)
+            most = fmaxf(most, __shfl_xor(most, s));
+        double sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            score[i] = v[i] > -INFINITY ? exp(static_cast<double>(v[i]) - static_cast<double>(most)) : 0.0;
+            sum += score[i];
+        }
+        sum = sum_lanes(sum);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            score[i] = score[i] / sum;
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            score[i] = 1.0 / (1.0 + exp(-static_cast<double>(v[i])));
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const double bias = a.bias && e0 + i < a.experts ? static_cast<double>(a.bias[e0 + i]) : 0.0;
+        // a value that is not a number (from the bias) counts as off, too
+        const double value = score[i] + bias;
+        key[i] = v[i] > -INFINITY && value > -INFINITY ? key_of(value) : 0;
+    }
+    if (a.groups > 1) {
+        // every group is looked through by `lanes` lanes
+        uint64_t *mine = lds + wave * PER * 64;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            mine[e0 + i] = key[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int lanes = a.group_lanes, g = lane / lanes, first = lane % lanes;
+        uint64_t best = 0, next = 0;
+        if (g < a.groups)
+            for (int i = first; i < a.each; i += lanes) {
+                const uint64_t k = mine[g * a.each + i];
+                next = max(next, min(best, k));
+                best = max(best, k);
+            }
+        for (int s = 1; s < lanes; s *= 2) {
+            const uint64_t b = __shfl_xor(best, s), m = __shfl_xor(next, s);
+            next = max(max(next, m), min(best, b));
+            best = max(best, b);
+        }
+        uint64_t rank = 0;
+        if (best)
+            rank = key_of(value_of(best) + (a.group_top > 1 && next ? value_of(next) : 0.0));
+        int ahead = 0;  // groups that come before this lane's
+        for (int o = 0; o < a.groups; ++o) {
+            const uint64_t r = __shfl(rank, o * lanes);
+            ahead += r > rank || (r == rank && o < g);
+        }
+        const uint64_t kept = __ballot(g < a.groups && first == 0 && ahead < a.groups_kept);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t of = static_cast<uint32_t>(e0 + i) * a.each_inverse >> 20;
+            if (!(kept >> (of * lanes & 63) & 1))
+                key[i] = 0;
+        }
+    }
+    int32_t id = -1;
+    double weight = 0, sum = 0;
+    for (int j = 0; j < a.k; ++j) {
+        uint64_t best = key[0];
+        int at = 0;
+        double s = score[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) {
+            const bool more = key[i] > best;
+            best = more ? key[i] : best;
+            at = more ? i : at;
+            s = more ? score[i] : s;
+        }
+        uint64_t holders;
+        if (key_max(best, &holders) == 0)
+            break;
+        const int winner = __ffsll(static_cast<unsigned long long>(holders)) - 1;
+        const double chosen = lane_value(s, winner);
+        const int32_t which = winner * PER + __builtin_amdgcn_readlane(at, winner);
+        if (lane == j) {
+            id = which;
+            weight = chosen;
+        }
+        sum += chosen;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (which == e0 + i)
+                key[i] = 0;
+    }
+    if (lane < a.k) {
+        if (a.renorm)
+            weight = sum > 0 ? weight / sum : 0.0;
+        const int64_t to = static_cast<int64_t>(token) * a.k + lane;
+        a.ids[to] = id;
+        a.weights[to] = static_cast<float>(weight * static_cast<double>(a.factor));
+    }
+}
+
+// Rows by expert: workgroup e finds the places of expert e's pairs (token,
+// choice) in the order of all pairs sorted by expert.  It counts, over all
+// pairs, those of lower experts (its first place) and its own, then hands out
+// its places in the order of the pairs; no workgroup waits for another.
+__global__ void __launch_bounds__(1024) sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order,
+                                                   int32_t *place, int32_t *offsets) {
+    __shared__ int32_t part[2][16];
+    const int32_t e = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int32_t per = (pairs + blockDim.x - 1) / static_cast<int32_t>(blockDim.x);
+    const int32_t first = min(static_cast<int64_t>(threadIdx.x) * per, static_cast<int64_t>(pairs));
+    const int32_t last = min(static_cast<int64_t>(first) + per, static_cast<int64_t>(pairs));
+    int32_t below = 0, own = 0;
+    for (int32_t i = first; i < last; ++i) {
+        const int32_t id = ids[i];
+        below += id >= 0 && id < e;
+        own += id == e;
+        if (e == 0 && (id < 0 || id >= experts))
+            place[i] = -1;
+    }
+    int32_t upto = own;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int32_t o = __shfl_up(upto, s);
+        upto += lane >= s ? o : 0;
+        below += __shfl_xor(below, s);
+    }
+    if (lane == 63) {
+        part[0][wave] = upto;
+        part[1][wave] = below;
+    }
+    __syncthreads();
+    int32_t start = 0, total = 0;
+    for (int w = 0; w < waves; ++w) {
+        start += part[1][w] + (w < wave ? part[0][w] : 0);
+        total += part[1][w] + part[0][w];
+    }
+    if (threadIdx.x == 0) {
+        offsets[e + 1] = total;
+        if (e == 0)
+            offsets[0] = 0;
+    }
+    int32_t at = start + upto - own;
+    for (int32_t i = first; i < last; ++i)
+        if (ids[i] == e) {
+            order[at] = i;
+            place[i] = at++;
+        }
+}
+
+template <typename T, int PER>
+hipError_t route_per(const RouteArgs &a, hipStream_t stream) {
+    const int64_t piece = static_cast<int64_t>(sizeof(T)) * PER;
+    const bool wide = reinterpret_cast<uintptr_t>(a.logits) % std::min<int64_t>(piece, 16) == 0 &&
+                      a.ld * static_cast<int64_t>(sizeof(T)) % std::min<int64_t>(piece, 16) == 0;
+    const size_t lds = a.groups > 1 ? 4 * PER * 64 * 8 : 0;
+    route_kernel<T, PER><<<(a.n + 3) / 4, 256, lds, stream>>>(a, wide);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t route_of(const RouteArgs &a, hipStream_t stream) {
+    return a.experts <= 64    ? route_per<T, 1>(a, stream)
+           : a.experts <= 128 ? route_per<T, 2>(a, stream)
+           : a.experts <= 256 ? route_per<T, 4>(a, stream)
+           : a.experts <= 512 ? route_per<T, 8>(a, stream)
+                              : route_per<T, 16>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_route(RouteArgs a, int32_t type, hipStream_t stream) {
+    a.each = a.experts / a.groups;
+    a.each_inverse = ((1u << 20) + a.each - 1) / a.each;  // e * this >> 20 = e / each below 1024
+    a.group_lanes = 1;
+    while (a.group_lanes * 2 * a.groups <= 64)
+        a.group_lanes *= 2;
+    return type == kF32 ? route_of<float>(a, stream)
+           : type == kF16 ? route_of<_Float16>(a, stream)
+                          : route_of<__bf16>(a, stream);
+}
+
+hipError_t launch_sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order, int32_t *place,
+                             int32_t *offsets, hipStream_t stream) {
+    const int32_t threads = pairs >= 4096 ? 1024 : 256;
+    sort_pairs<<<experts, threads, 0, stream>>>(ids, pairs, experts, order, place, offsets);
+    return hipGetLastError();
+}
+
+}  // namespace spconv

@@ -1,4 +1,4 @@
-"""Dense layers in 8 bits, for torch tensors.
+"""Dense layers in 8 bits, routers and experts, for torch tensors.
 
 The arithmetic runs in libspconv's kernels (include/spconv.h says what each
 computes and how its arrays are laid out); this module checks shapes, types and
@@ -13,7 +13,8 @@ before the other stream is done with it.
 
 from __future__ import annotations
 
-from .spconv import (BF16, F16, F32, FP8, spconv_linear_fp8, spconv_linear_fp8_workspace, spconv_quantize_fp8)
+from .spconv import (BF16, F16, F32, FP8, spconv_experts_fp8, spconv_experts_fp8_workspace, spconv_linear_fp8,
+                     spconv_linear_fp8_workspace, spconv_quantize_fp8, spconv_route)
 
 BLOCK = 128
 _TYPES = {}
@@ -130,4 +131,96 @@ class Fp8Linear:
         if n:
             spconv_linear_fp8(x, kind, ld, x_scale, self.w, self.w_scale, self.bias, self.act, y, _type(y, "y"), n,
                               self.cin, self.cout, workspace if size else None, size, stream)
+        return y
+
+
+def route(logits, k: int, score: str = "softmax", bias=None, groups: int = 1, groups_kept: int = 1,
+          group_top: int = 1, renorm: bool = True, factor: float = 1.0, ids=None, weights=None, stream=None):
+    """The k experts (int32) of each token and their weights (float32), both
+    [n, k], from a router's logits [n, experts]; spconv_route in
+    include/spconv.h defines them."""
+    import torch
+    kind = _type(logits, "logits")
+    n, experts, ld = _matrix(logits, "logits")
+    if score not in ("softmax", "sigmoid"):
+        raise ValueError("score must be 'softmax' or 'sigmoid'")
+    dev = logits.device
+    if bias is not None:
+        _given(bias, (experts,), torch.float32, dev, "bias")
+    if ids is None:
+        ids = torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
+    else:
+        _given(ids, (n, k), torch.int32, dev, "ids")
+    if weights is None:
+        weights = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev)
+    else:
+        _given(weights, (n, k), torch.float32, dev, "weights")
+    spconv_route(logits, kind, ld, bias, score, n, experts, groups, groups_kept, group_top, k, renorm, factor, ids,
+                 weights, stream)
+    return ids, weights
+
+
+class Experts:
+    """The gated feed-forward networks of a layer's experts, in 8 bits: codes
+    and scales of W1 and W3 [experts, 2, inner, hidden] and of W2 [experts,
+    hidden, inner], each matrix quantised by 128 x 128 blocks of its own.  It
+    keeps the tensors given."""
+
+    def __init__(self, w13, w13_scale, w2, w2_scale, hidden: int, inner: int):
+        import torch
+        f8, f32, dev = torch.float8_e4m3fn, torch.float32, w13.device
+        hb, ib, e = _blocks(hidden), _blocks(inner), int(w13.shape[0])
+        self.w13 = _given(w13, (e, 2, inner, hb * BLOCK), f8, dev, "w13")
+        self.w13_scale = _given(w13_scale, (e, 2, ib, hb), f32, dev, "w13_scale")
+        self.w2 = _given(w2, (e, hidden, ib * BLOCK), f8, dev, "w2")
+        self.w2_scale = _given(w2_scale, (e, hb, ib), f32, dev, "w2_scale")
+        self.experts, self.hidden, self.inner = e, int(hidden), int(inner)
+
+    @classmethod
+    def from_dense(cls, w1, w3, w2):
+        """The experts of W1 and W3 [experts, inner, hidden] and W2 [experts,
+        hidden, inner] in float32, float16 or bfloat16."""
+        import torch
+        e, inner, hidden = w1.shape
+        hb, ib = _blocks(hidden), _blocks(inner)
+        f8, f32, dev = torch.float8_e4m3fn, torch.float32, w1.device
+        w13 = torch.empty((e, 2, inner, hb * BLOCK), dtype=f8, device=dev)
+        w13_scale = torch.empty((e, 2, ib, hb), dtype=f32, device=dev)
+        q2 = torch.empty((e, hidden, ib * BLOCK), dtype=f8, device=dev)
+        q2_scale = torch.empty((e, hb, ib), dtype=f32, device=dev)
+        for i in range(e):
+            quantize_fp8(w1[i], BLOCK, w13[i, 0], w13_scale[i, 0])
+            quantize_fp8(w3[i], BLOCK, w13[i, 1], w13_scale[i, 1])
+            quantize_fp8(w2[i], BLOCK, q2[i], q2_scale[i])
+        return cls(w13, w13_scale, q2, q2_scale, hidden, inner)
+
+    def workspace_bytes(self, n: int, k: int) -> int:
+        """Workspace of run() for n tokens of k experts."""
+        return spconv_experts_fp8_workspace(n, k, self.experts, self.hidden, self.inner)
+
+    def run(self, x, ids, weights, y=None, workspace=None, stream=None):
+        """y [n, hidden] = the sum of the experts' outputs for x [n, hidden],
+        with ids (int32) and weights (float32) [n, k] as route() gives them."""
+        import torch
+        dev = self.w13.device
+        kind = _type(x, "x")
+        n, cols, ld = _matrix(x, "x")
+        if cols != self.hidden or x.device != dev:
+            raise ValueError("x must have %d channels and be on %s" % (self.hidden, dev))
+        if ids.dim() != 2:
+            raise ValueError("ids must be a matrix [n, k]")
+        k = int(ids.shape[1])
+        _given(ids, (n, k), torch.int32, dev, "ids")
+        _given(weights, (n, k), torch.float32, dev, "weights")
+        if y is None:
+            y = torch.empty((n, cols), dtype=x.dtype, device=dev)
+        else:
+            _given(y, (n, cols), x.dtype, dev, "y")
+        if workspace is None:
+            size = self.workspace_bytes(n, k)
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        else:
+            size = workspace.numel() * workspace.element_size()
+        spconv_experts_fp8(x, kind, ld, ids, weights, self.w13, self.w13_scale, self.w2, self.w2_scale, y, n, k,
+                           self.experts, self.hidden, self.inner, workspace, size, stream)
         return y

@@ -36,7 +36,7 @@ EXPORTED = ("spconv_plan_create", "spconv_run", "spconv_destroy", "spconv_last_e
             "spconv_dense_to_bcsr_blocked", "spconv_plan_create_dense_blocked", "spconv_plan_unpack_indexed",
             "spconv_plan_check", "spconv_plan_set_wait_limit", "spconv_plan_create_static",
             "spconv_plan_unpack_outer", "spconv_plan_run_kernel", "spconv_quantize_fp8", "spconv_linear_fp8",
-            "spconv_linear_fp8_workspace")
+            "spconv_linear_fp8_workspace", "spconv_route", "spconv_experts_fp8", "spconv_experts_fp8_workspace")
 
 
 class SpconvError(RuntimeError):
@@ -158,6 +158,12 @@ def load_library(path: Optional[str] = None):
     lib.spconv_linear_fp8.argtypes = [vp, i32, i64, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, vp, i64, vp]
     lib.spconv_linear_fp8_workspace.restype = i32
     lib.spconv_linear_fp8_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.spconv_route.restype = i32
+    lib.spconv_route.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp]
+    lib.spconv_experts_fp8.restype = i32
+    lib.spconv_experts_fp8.argtypes = [vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp]
+    lib.spconv_experts_fp8_workspace.restype = i32
+    lib.spconv_experts_fp8_workspace.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
     if path is None:
         _lib = lib
     return lib
@@ -466,6 +472,42 @@ def spconv_linear_fp8_workspace(x_dtype, n, cin, cout) -> int:
     b = ctypes.c_int64()
     _check(load_library().spconv_linear_fp8_workspace(_op_dtype(x_dtype), int(n), int(cin), int(cout),
                                                       ctypes.byref(b)))
+    return b.value
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def spconv_route(logits, dtype, ld, bias, score, n, experts, groups, groups_kept, group_top, k, renorm, factor, ids,
+                 weights, stream=None, check: bool = True):
+    """Queue a router: the k experts of each token and their weights."""
+    s = _SCORES[score] if isinstance(score, str) else int(score)
+    status = load_library().spconv_route(_devptr(logits), _op_dtype(dtype), int(ld), _devptr(bias), s, int(n),
+                                         int(experts), int(groups), int(groups_kept), int(group_top), int(k),
+                                         int(bool(renorm)), float(factor), _devptr(ids), _devptr(weights),
+                                         _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_experts_fp8(x, dtype, ldx, ids, weights, w13, w13_scale, w2, w2_scale, y, n, k, experts, hidden, inner,
+                       workspace, workspace_bytes, stream=None, check: bool = True):
+    """Queue the chosen experts' gated feed-forward networks on 8-bit weights."""
+    status = load_library().spconv_experts_fp8(_devptr(x), _op_dtype(dtype), int(ldx), _devptr(ids), _devptr(weights),
+                                               _devptr(w13), _devptr(w13_scale), _devptr(w2), _devptr(w2_scale),
+                                               _devptr(y), int(n), int(k), int(experts), int(hidden), int(inner),
+                                               _devptr(workspace), int(workspace_bytes), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_experts_fp8_workspace(n, k, experts, hidden, inner) -> int:
+    """Bytes of workspace that spconv_experts_fp8 needs."""
+    b = ctypes.c_int64()
+    _check(load_library().spconv_experts_fp8_workspace(int(n), int(k), int(experts), int(hidden), int(inner),
+                                                       ctypes.byref(b)))
     return b.value
 
 
