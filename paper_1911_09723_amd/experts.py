@@ -13,32 +13,42 @@ before the other stream is done with it.
 
 from __future__ import annotations
 
-from .spconv import (BF16, F16, F32, FP8, spconv_experts_fp8, spconv_experts_fp8_workspace, spconv_linear_fp8,
-                     spconv_linear_fp8_workspace, spconv_quantize_fp8, spconv_route)
+from functools import lru_cache
+
+from .spconv import (_ACTS, _SCORES, BF16, F16, F32, FP8, _check, _stream, load_library,
+                     spconv_experts_fp8_workspace, spconv_linear_fp8_workspace)
 
 BLOCK = 128
 _TYPES = {}
+# sizes are asked for on every call
+_linear_workspace = lru_cache(maxsize=1024)(spconv_linear_fp8_workspace)
+_experts_workspace = lru_cache(maxsize=1024)(spconv_experts_fp8_workspace)
 
 
-def _type(t, what: str) -> int:
-    """The library's number for a tensor's element type."""
+def _type(dtype, what: str) -> int:
+    """The library's number for a torch element type."""
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
     try:
-        return _TYPES[t.dtype]
+        return _TYPES[dtype]
     except KeyError:
-        raise ValueError("%s must be float32, float16 or bfloat16, not %s" % (what, t.dtype)) from None
+        raise ValueError("%s must be float32, float16 or bfloat16, not %s" % (what, dtype)) from None
 
 
 def _matrix(x, what: str):
-    """(rows, cols, row stride) of a matrix on the GPU whose rows are contiguous."""
-    if x.dim() != 2 or not x.is_cuda:
-        raise ValueError("%s must be a matrix on the GPU" % what)
+    """(rows, cols, row stride) of a matrix on the current GPU whose rows are contiguous."""
+    if x.dim() != 2 or not x.is_cuda or x.get_device() != _current_device():
+        raise ValueError("%s must be a matrix on the current GPU" % what)
     rows, cols = x.shape
     if cols > 1 and x.stride(1) != 1:
         raise ValueError("%s must have contiguous rows" % what)
     return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
 
 
 def _given(t, shape, dtype, device, what: str):
@@ -57,22 +67,23 @@ def quantize_fp8(x, block_rows: int = 1, q=None, scale=None, stream=None):
     ceil(cols / 128)) and scales: [kb, rows] with block_rows = 1 (activations),
     [ceil(rows / 128), kb] with block_rows = 128 (weights)."""
     import torch
-    kind = _type(x, "x")
+    kind = _type(x.dtype, "x")
     rows, cols, ld = _matrix(x, "x")
     if block_rows not in (1, BLOCK):
         raise ValueError("block_rows must be 1 or %d" % BLOCK)
     kb = _blocks(cols)
     shape, codes = (kb, rows) if block_rows == 1 else (_blocks(rows), kb), (rows, kb * BLOCK)
     if q is None:
-        q = torch.empty(codes, dtype=torch.float8_e4m3fn, device=x.device)
+        q = x.new_empty(codes, dtype=torch.float8_e4m3fn)
     else:
         _given(q, codes, torch.float8_e4m3fn, x.device, "q")
     if scale is None:
-        scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+        scale = x.new_empty(shape, dtype=torch.float32)
     else:
         _given(scale, shape, torch.float32, x.device, "scale")
     if rows and cols:
-        spconv_quantize_fp8(x, kind, ld, rows, cols, block_rows, q, scale, stream)
+        _check(load_library().spconv_quantize_fp8(x.data_ptr(), kind, ld, rows, cols, block_rows, q.data_ptr(),
+                                                  scale.data_ptr(), _stream(stream)))
     return q, scale
 
 
@@ -98,8 +109,7 @@ class Fp8Linear:
 
     def workspace_bytes(self, n: int, dtype) -> int:
         """Workspace of run() for n rows of a torch dtype that is not quantised yet."""
-        import torch
-        return spconv_linear_fp8_workspace(_type(torch.empty(0, dtype=dtype), "x"), n, self.cin, self.cout)
+        return _linear_workspace(_type(dtype, "x"), n, self.cin, self.cout)
 
     def run(self, x, x_scale=None, y=None, dtype=None, workspace=None, stream=None):
         """y [n, cout] for x [n, cin], or for quantize_fp8's codes and scales
@@ -107,7 +117,7 @@ class Fp8Linear:
         import torch
         dev = self.w.device
         if x_scale is None:
-            kind = _type(x, "x")
+            kind = _type(x.dtype, "x")
             n, cols, ld = _matrix(x, "x")
             if cols != self.cin or x.device != dev:
                 raise ValueError("x must have %d channels and be on %s" % (self.cin, dev))
@@ -120,17 +130,20 @@ class Fp8Linear:
                 raise ValueError("quantised rows need y or its dtype")
             dtype = dtype or y.dtype
         if y is None:
-            y = torch.empty((n, self.cout), dtype=dtype, device=dev)
+            y = x.new_empty((n, self.cout), dtype=dtype)
         else:
             _given(y, (n, self.cout), dtype, dev, "y")
-        size = spconv_linear_fp8_workspace(kind, n, self.cin, self.cout)
+        size = _linear_workspace(kind, n, self.cin, self.cout)
         if size and workspace is None:
-            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+            workspace = x.new_empty(size, dtype=torch.uint8)
         elif size:
             size = workspace.numel() * workspace.element_size()
         if n:
-            spconv_linear_fp8(x, kind, ld, x_scale, self.w, self.w_scale, self.bias, self.act, y, _type(y, "y"), n,
-                              self.cin, self.cout, workspace if size else None, size, stream)
+            _check(load_library().spconv_linear_fp8(
+                x.data_ptr(), kind, ld, None if x_scale is None else x_scale.data_ptr(),
+                self.w.data_ptr(), self.w_scale.data_ptr(), None if self.bias is None else self.bias.data_ptr(),
+                _ACTS[self.act], y.data_ptr(), _type(y.dtype, "y"), n, self.cin, self.cout, workspace.data_ptr() if size else None, size,
+                _stream(stream)))
         return y
 
 
@@ -140,23 +153,23 @@ def route(logits, k: int, score: str = "softmax", bias=None, groups: int = 1, gr
     [n, k], from a router's logits [n, experts]; spconv_route in
     include/spconv.h defines them."""
     import torch
-    kind = _type(logits, "logits")
+    kind = _type(logits.dtype, "logits")
     n, experts, ld = _matrix(logits, "logits")
     if score not in ("softmax", "sigmoid"):
         raise ValueError("score must be 'softmax' or 'sigmoid'")
-    dev = logits.device
     if bias is not None:
-        _given(bias, (experts,), torch.float32, dev, "bias")
+        _given(bias, (experts,), torch.float32, logits.device, "bias")
     if ids is None:
-        ids = torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
+        ids = logits.new_empty((n, max(k, 0)), dtype=torch.int32)
     else:
-        _given(ids, (n, k), torch.int32, dev, "ids")
+        _given(ids, (n, k), torch.int32, logits.device, "ids")
     if weights is None:
-        weights = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev)
+        weights = logits.new_empty((n, max(k, 0)), dtype=torch.float32)
     else:
-        _given(weights, (n, k), torch.float32, dev, "weights")
-    spconv_route(logits, kind, ld, bias, score, n, experts, groups, groups_kept, group_top, k, renorm, factor, ids,
-                 weights, stream)
+        _given(weights, (n, k), torch.float32, logits.device, "weights")
+    _check(load_library().spconv_route(
+        logits.data_ptr(), kind, ld, None if bias is None else bias.data_ptr(), _SCORES[score], n, experts, groups,
+        groups_kept, group_top, k, renorm, factor, ids.data_ptr(), weights.data_ptr(), _stream(stream)))
     return ids, weights
 
 
@@ -196,14 +209,14 @@ class Experts:
 
     def workspace_bytes(self, n: int, k: int) -> int:
         """Workspace of run() for n tokens of k experts."""
-        return spconv_experts_fp8_workspace(n, k, self.experts, self.hidden, self.inner)
+        return _experts_workspace(n, k, self.experts, self.hidden, self.inner)
 
     def run(self, x, ids, weights, y=None, workspace=None, stream=None):
         """y [n, hidden] = the sum of the experts' outputs for x [n, hidden],
         with ids (int32) and weights (float32) [n, k] as route() gives them."""
         import torch
         dev = self.w13.device
-        kind = _type(x, "x")
+        kind = _type(x.dtype, "x")
         n, cols, ld = _matrix(x, "x")
         if cols != self.hidden or x.device != dev:
             raise ValueError("x must have %d channels and be on %s" % (self.hidden, dev))
@@ -213,14 +226,16 @@ class Experts:
         _given(ids, (n, k), torch.int32, dev, "ids")
         _given(weights, (n, k), torch.float32, dev, "weights")
         if y is None:
-            y = torch.empty((n, cols), dtype=x.dtype, device=dev)
+            y = x.new_empty((n, cols))
         else:
             _given(y, (n, cols), x.dtype, dev, "y")
         if workspace is None:
             size = self.workspace_bytes(n, k)
-            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+            workspace = x.new_empty(size, dtype=torch.uint8)
         else:
             size = workspace.numel() * workspace.element_size()
-        spconv_experts_fp8(x, kind, ld, ids, weights, self.w13, self.w13_scale, self.w2, self.w2_scale, y, n, k,
-                           self.experts, self.hidden, self.inner, workspace, size, stream)
+        _check(load_library().spconv_experts_fp8(
+            x.data_ptr(), kind, ld, ids.data_ptr(), weights.data_ptr(), self.w13.data_ptr(), self.w13_scale.data_ptr(),
+            self.w2.data_ptr(), self.w2_scale.data_ptr(), y.data_ptr(), n, k, self.experts, self.hidden, self.inner,
+            workspace.data_ptr(), size, _stream(stream)))
         return y

@@ -166,6 +166,7 @@ def load_library(path: Optional[str] = None):
     lib.spconv_experts_fp8_workspace.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
     if path is None:
         _lib = lib
+        _bind_current_stream()
     return lib
 
 
@@ -394,10 +395,26 @@ def spconv_run(plan, x, y, n, h, w, stream=None, check: bool = True):
     return status
 
 
+def _current_stream() -> int:
+    """Torch's current stream on the current device (2.6 us through a Stream object)."""
+    import torch
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _bind_current_stream():
+    """Replace _current_stream by torch's raw-handle query (0.3 us) where this torch has it."""
+    global _current_stream
+    try:
+        from torch._C import _cuda_getCurrentRawStream as raw
+        from torch.cuda import current_device
+    except ImportError:
+        return
+    _current_stream = lambda: raw(current_device())  # noqa: E731
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
