@@ -329,8 +329,8 @@ SPCONV_API spconv_status spconv_quantize_fp8(const void *x, spconv_dtype dtype, 
  * n == 0 or cout == 0 is a no-op.
  * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
  * cin, bad dtype, act or alignment, x_scale missing or not asked for, workspace
- * too small, overlap), SPCONV_E_SHAPE (cin == 0 with outputs, cin above 2^24, n
- * * ceil(cin / 128) of 2^27 or more, n * cout of 2^36 or more), SPCONV_E_HIP.
+ * too small, overlap), SPCONV_E_SHAPE (cin == 0 with outputs, cin or cout above 2^22,
+ * n * ceil(cin / 128) of 2^27 or more, n * cout of 2^36 or more), SPCONV_E_HIP.
  */
 SPCONV_API spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx, const float *x_scale,
                                            const void *w, const float *w_scale, const float *bias, spconv_act act,
@@ -403,7 +403,7 @@ SPCONV_API spconv_status spconv_route(const void *logits, spconv_dtype dtype, in
  * Errors: SPCONV_E_ARG (NULL pointer with work to do, bad dtype or alignment,
  * negative size, k < 1, ldx < hidden, workspace too small, overlap),
  * SPCONV_E_SHAPE (experts, hidden or inner < 1, n * k * max(ceil(hidden / 128),
- * ceil(inner / 128)) of 2^27 or more), SPCONV_E_UNSUPPORTED (more than 1024
+ * ceil(inner / 128)) of 2^25 or more), SPCONV_E_UNSUPPORTED (more than 1024
  * experts, k > 64, hidden or inner above 32768), SPCONV_E_HIP.
  */
 SPCONV_API spconv_status spconv_experts_fp8(const void *x, spconv_dtype dtype, int64_t ldx, const int32_t *ids,

@@ -18,7 +18,8 @@ using spconv::set_error;
 
 constexpr int64_t kMostBlocks = int64_t(1) << 27;  // row blocks of a matrix: launches stay below 2^32 threads
 constexpr int64_t kMostOutputs = int64_t(1) << 36;
-constexpr int32_t kMostChannels = 1 << 24;
+constexpr int32_t kMostChannels = 1 << 22;          // a tile of 256 rows lies within 32-bit offsets
+constexpr int64_t kMostExpertBlocks = int64_t(1) << 25;  // rows by token and by pair lie within 32-bit offsets
 
 bool is_float(int32_t type) { return type == SPCONV_F32 || type == SPCONV_F16 || type == SPCONV_BF16; }
 int64_t size_of(int32_t type) { return type == SPCONV_F32 ? 4 : type == SPCONV_FP8 ? 1 : 2; }
@@ -74,7 +75,7 @@ spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t
     if (cin == 0)
         return set_error(SPCONV_E_SHAPE, "cin must be >= 1");
     if (cin > kMostChannels || cout > kMostChannels)
-        return set_error(SPCONV_E_SHAPE, "cin and cout must be at most 2^24");
+        return set_error(SPCONV_E_SHAPE, "cin and cout must be at most 2^22");
     if (static_cast<int64_t>(n) * blocks_of(cin) >= kMostBlocks)
         return set_error(SPCONV_E_SHAPE, "n * ceil(cin / 128) must be below 2^27");
     if (static_cast<int64_t>(n) * cout >= kMostOutputs)
@@ -100,8 +101,8 @@ spconv_status check_experts(int32_t n, int32_t k, int32_t experts, int32_t hidde
         return set_error(SPCONV_E_UNSUPPORTED, "at most 1024 experts and k = 64 are supported");
     if (hidden > kMostExpertChannels || inner > kMostExpertChannels)
         return set_error(SPCONV_E_UNSUPPORTED, "hidden and inner must be at most 32768");
-    if (static_cast<int64_t>(n) * k * blocks_of(hidden > inner ? hidden : inner) >= kMostBlocks)
-        return set_error(SPCONV_E_SHAPE, "n * k * ceil(channels / 128) must be below 2^27");
+    if (static_cast<int64_t>(n) * k * blocks_of(hidden > inner ? hidden : inner) >= kMostExpertBlocks)
+        return set_error(SPCONV_E_SHAPE, "n * k * ceil(channels / 128) must be below 2^25");
     return SPCONV_OK;
 }
 

@@ -87,28 +87,30 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     int32_t fb;
     if (!find_tile(a.offsets, a.experts, S::BT, columns, lane, &tile, &fb))
         return;
-    const int64_t pitch = static_cast<int64_t>(a.hb) * kBlock;
-    const uint8_t *w = a.w13 + static_cast<int64_t>(tile.expert) * 2 * a.inner * pitch;
+    const uint32_t pitch = a.hb * kBlock;
     const float *ws = a.s13 + static_cast<int64_t>(tile.expert) * 2 * a.ib * a.hb + static_cast<int64_t>(fb) * a.hb;
-    const uint8_t *src[S::kLoads];
+    TileSource<S> from;
+    from.w = a.w13 + static_cast<int64_t>(tile.expert) * 2 * a.inner * pitch;
+    from.w_bytes = 2 * a.inner * pitch;
+    from.x = a.xq;
+    from.x_bytes = a.n * pitch;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        const uint8_t *row;
+        uint32_t row;
         if (line < S::BC) {  // lines of a wavefront: 64 gate, then 64 up channels
-            const int32_t ch = min(fb * kBlock + line / 128 * 64 + line % 64, a.inner - 1);
-            row = w + (ch + (line & 64 ? a.inner : 0)) * pitch;
+            row = min(fb * kBlock + line / 128 * 64 + line % 64, a.inner - 1) + (line & 64 ? a.inner : 0);
         } else {
-            const int32_t pair = a.order[tile.row + min(line - S::BC, tile.rows - 1)];
-            row = a.xq + (pair / a.k) * pitch;
+            row = a.order[tile.row + min(line - S::BC, tile.rows - 1)] / a.k;
         }
-        src[i] = row + tile_byte(line, lane);
+        from.at[i] = row * pitch + tile_byte(line, lane);
     }
-    const float *xs = a.xs;
-    if (wave < S::BT / 64)
-        xs += a.order[tile.row + min(wave * 64 + lane, tile.rows - 1)] / a.k;
+    from.xs = a.xs;
+    from.xs_at = wave < S::BT / 64 ? a.order[tile.row + min(wave * 64 + lane, tile.rows - 1)] / a.k * 4u : 0;
+    from.xs_step = a.n * 4u;
+    from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, true>(acc, src, xs, a.n, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
+    tile_product<S, EXACT, true>(acc, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
 
     const int wc = wave / S::WT, wt = wave % S::WT;
     float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
@@ -164,22 +166,27 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
     if (!find_tile(a.offsets, a.experts, S::BT, columns, lane, &tile, &ct))
         return;
     const int32_t c0 = ct * S::BC;
-    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
-    const uint8_t *w = a.w2 + static_cast<int64_t>(tile.expert) * a.hidden * pitch;
-    const uint8_t *src[S::kLoads];
+    const uint32_t pitch = a.ib * kBlock;
+    TileSource<S> from;
+    from.w = a.w2 + (static_cast<int64_t>(tile.expert) * a.hidden + c0) * pitch;
+    from.w_bytes = min(S::BC, a.hidden - c0) * pitch;
+    from.x = a.hq + static_cast<int64_t>(tile.row) * pitch;
+    from.x_bytes = tile.rows * pitch;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        const uint8_t *row = line < S::BC ? w + min(c0 + line, a.hidden - 1) * pitch
-                                          : a.hq + (tile.row + min(line - S::BC, tile.rows - 1)) * pitch;
-        src[i] = row + tile_byte(line, lane);
+        const int row = line < S::BC ? min(line, a.hidden - 1 - c0) : min(line - S::BC, tile.rows - 1);
+        from.at[i] = row * pitch + tile_byte(line, lane);
     }
+    from.xs = a.hs + tile.row;
+    from.xs_at = min(wave * 64 + lane, tile.rows - 1) * 4u;
+    from.xs_step = a.pairs * 4u;
+    from.xs_bytes = from.xs_step * (a.ib - 1) + tile.rows * 4u;
     const int wc = wave / S::WT, wt = wave % S::WT;
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + min(cw, a.hidden - 1) / kBlock) * a.ib;
-    const float *xs = a.hs + tile.row + min(wave * 64 + lane, tile.rows - 1);
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, false>(acc, src, xs, a.pairs, ws, nullptr, a.ib, lds, wave, lane);
+    tile_product<S, EXACT, false>(acc, from, ws, nullptr, a.ib, lds, wave, lane);
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
 #pragma unroll
@@ -459,12 +466,15 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
     } else {
         using Small = TileShape<256, 64, 2, 4>;
         using Mid = TileShape<256, 128, 2, 4>;
-        const bool high = a.pairs > 96ll * a.experts;
+        using Big = TileShape<256, 256, 2, 4>;
+        const int64_t each = a.pairs / a.experts;
         if ((e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
             return e;
         // bf16: what the 8-bit instruction loses lies below the rounding of the result
         if (a.type == kBf16)
-            e = high ? gated_tiles<Mid, false>(a, stream) : gated_tiles<Small, false>(a, stream);
+            e = each >= 192  ? gated_tiles<Big, false>(a, stream)
+                : each >= 96 ? gated_tiles<Mid, false>(a, stream)
+                             : gated_tiles<Small, false>(a, stream);
         else
             e = gated_tiles<Small, true>(a, stream);
         if (e != hipSuccess)
@@ -472,7 +482,9 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         if (a.type == kF32)
             e = down_tiles<TileShape<128, 128, 2, 2>, true>(a, stream);
         else
-            e = high ? down_tiles<Mid, false>(a, stream) : down_tiles<Small, false>(a, stream);
+            e = each >= 192  ? down_tiles<Big, false>(a, stream)
+                : each >= 96 ? down_tiles<Mid, false>(a, stream)
+                             : down_tiles<Small, false>(a, stream);
     }
     if (e != hipSuccess)
         return e;

@@ -40,22 +40,28 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     const int32_t group = id / (8 * ctiles), high = min(8, ttiles - 8 * group), in = id - group * 8 * ctiles;
     const int32_t ct = in / high, tt = group * 8 + in - ct * high;
     const int32_t c0 = ct * S::BC, t0 = tt * S::BT;
-    const int64_t pitch = static_cast<int64_t>(a.kb) * kBlock;
-    const uint8_t *src[S::kLoads];
+    const uint32_t pitch = a.kb * kBlock;
+    TileSource<S> from;
+    from.w = a.w + static_cast<int64_t>(c0) * pitch;
+    from.x = static_cast<const uint8_t *>(a.x) + static_cast<int64_t>(t0) * pitch;
+    from.w_bytes = min(S::BC, a.cout - c0) * pitch;
+    from.x_bytes = min(S::BT, a.n - t0) * pitch;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
         // lines past the last row or channel repeat it: their results are not stored
-        const uint8_t *row = line < S::BC ? a.w + min(c0 + line, a.cout - 1) * pitch
-                                          : static_cast<const uint8_t *>(a.x) + min(t0 + line - S::BC, a.n - 1) * pitch;
-        src[i] = row + tile_byte(line, lane);
+        const int row = line < S::BC ? min(line, a.cout - 1 - c0) : min(line - S::BC, a.n - 1 - t0);
+        from.at[i] = row * pitch + tile_byte(line, lane);
     }
+    from.xs = a.xs;
+    from.xs_at = min(t0 + wave * 64 + lane, a.n - 1) * 4u;
+    from.xs_step = a.n * 4u;
+    from.xs_bytes = from.xs_step * a.kb;
     const int wc = wave / S::WT, wt = wave % S::WT;
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
-    const float *xs = a.xs + min(t0 + wave * 64 + lane, a.n - 1);
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, false>(acc, src, xs, a.n, ws, nullptr, a.kb, lds, wave, lane);
+    tile_product<S, EXACT, false>(acc, from, ws, nullptr, a.kb, lds, wave, lane);
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
 #pragma unroll

@@ -23,8 +23,22 @@ namespace spconv {
 //
 // A line's 16-byte pieces are stored in the order piece ^ (line / 2 % 8): 16
 // lanes that read one piece of 16 neighbouring lines then touch each of LDS's
-// 16-byte columns (256 bytes, two lines) once.  The permutation is done by the
-// loads' global addresses, within a line, since their LDS places are fixed.
+// 16-byte columns (256 bytes, two lines) once: no bank conflicts (counted).
+// The permutation is done by the loads' global addresses, within a line, since
+// their LDS places are fixed.
+//
+// Order of a block's instructions.  A load of 1 KiB to LDS takes about 17
+// cycles of the compute unit's address path, and a wavefront that issues its
+// loads in a row stands still for as long as all of them take (8 loads of 8
+// wavefronts: 1080 cycles, a third of the block).  They are issued one after
+// every second product instead, which also leaves them the rest of the block to
+// arrive.  The multiply-adds of a piece follow one column of pieces later than
+// its product, when the result is there.  The compiler would undo both (it
+// gathers the loads and lets each multiply-add wait for its product), hence the
+// scheduling barriers and the empty assembly that pins the sums.  8192 x 4096 ->
+// 4096 in this order: 128 us, without it 143 to 167 us; the multiply-adds cost
+// 10 us of that, and half of what is left over the products' own 70 us is the
+// start of each block, where all wavefronts read their first operands at once.
 // ---------------------------------------------------------------------------
 template <int BC_, int BT_, int WC_, int WT_>
 struct TileShape {
@@ -32,20 +46,20 @@ struct TileShape {
     static constexpr int kWaves = WC * WT, kThreads = 64 * kWaves;
     static constexpr int NC = BC / WC / 16, NT = BT / WT / 16;
     static constexpr int kLines = BC + BT;
-    static constexpr int kLoads = kLines / 8 / kWaves;  // 8 lines an instruction
+    static constexpr int kLoads = kLines / 8 / kWaves;       // 8 lines an instruction
+    static constexpr int kWeightLoads = BC / 8 / kWaves;     // the first of them: W's
+    static constexpr int kStep = NC * NT >= 2 * kLoads ? 2 : 1;  // products from load to load
     static constexpr int kStage = kLines * kBlock + BT * 4;
     static constexpr int kLds = 2 * kStage;
-    static_assert(kLines % (8 * kWaves) == 0 && BT % 64 == 0 && BT / 64 <= kWaves, "whole loads a wavefront");
+    static_assert(BC % (8 * kWaves) == 0 && BT % (8 * kWaves) == 0 && BT % 64 == 0 && BT / 64 <= kWaves &&
+                      NC * NT >= kLoads, "whole loads a wavefront");
 };
 
-__device__ __forceinline__ void to_lds(const void *from, unsigned char *lds) {
-    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(const_cast<void *>(from)),
-                                     (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
-}
+using Rsrc = __amdgpu_buffer_rsrc_t;
 
-__device__ __forceinline__ void to_lds4(const void *from, unsigned char *lds) {
-    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(const_cast<void *>(from)),
-                                     (__attribute__((address_space(3))) void *)lds, 4, 0, 0);
+__device__ __forceinline__ Rsrc make_rsrc(const void *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), static_cast<short>(0), static_cast<int>(bytes),
+                                             0x00020000);
 }
 
 // The line (0 .. BC + BT - 1, W's first) and the byte in it that this lane
@@ -56,56 +70,112 @@ __device__ __forceinline__ int tile_line(int wave, int lane, int i) {
 }
 __device__ __forceinline__ int tile_byte(int line, int lane) { return ((lane & 7) ^ (line >> 1 & 7)) * 16; }
 
-// acc[c][t] += the products over kb blocks.  src[i]: this lane's i-th line at
-// its byte, block 0; xs: this lane's row scale of block 0 (wavefronts below
-// BT / 64 only), xs_step floats from block to block; ws0, ws1: the scales by
-// block of the first and of the second half of the wavefront's channel pieces.
+// What a tile reads: W and X from their bases, this lane's offsets of its lines
+// (block 0); the rows' scales and this lane's offset there (wavefronts below
+// BT / 64 only), step bytes from block to block.  Bytes: what each base covers.
+template <class S>
+struct TileSource {
+    const uint8_t *w, *x;
+    const float *xs;
+    uint32_t w_bytes, x_bytes, xs_bytes, xs_step;
+    uint32_t at[S::kLoads], xs_at;
+};
+
+__device__ __forceinline__ float uniform_load(const float *p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(p));
+}
+
+// acc[c][t] += the products over kb blocks; ws0, ws1: the scales by block of
+// the first and of the second half (HALVES) of the wavefront's channel pieces.
 template <class S, bool EXACT, bool HALVES>
-__device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const uint8_t *(&src)[S::kLoads],
-                                             const float *xs, int64_t xs_step, const float *ws0, const float *ws1,
-                                             int32_t kb, unsigned char *lds, int wave, int lane) {
+__device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const TileSource<S> &from, const float *ws0,
+                                             const float *ws1, int32_t kb, unsigned char *lds, int wave, int lane) {
     const int wc = wave / S::WT, wt = wave % S::WT;
-    auto stage = [&](int32_t b, unsigned char *buf) {
+    auto load = [&](int i, Rsrc w, Rsrc x, int32_t b, unsigned char *buf) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            i < S::kWeightLoads ? w : x,
+            (__attribute__((address_space(3))) void *)(buf + (wave + i * S::kWaves) * 1024), 16, from.at[i], b * kBlock, 0,
+            0);
+    };
+    auto load_scales = [&](Rsrc xs, int32_t b, unsigned char *buf) {
+        if (wave < S::BT / 64)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                xs, (__attribute__((address_space(3))) void *)(buf + S::kLines * kBlock + wave * 256), 4, from.xs_at,
+                b * from.xs_step, 0, 0);
+    };
+    {
+        const Rsrc w = make_rsrc(from.w, from.w_bytes), x = make_rsrc(from.x, from.x_bytes);
 #pragma unroll
         for (int i = 0; i < S::kLoads; ++i)
-            to_lds(src[i] + static_cast<int64_t>(b) * kBlock, buf + (wave + i * S::kWaves) * 1024);
-        if (wave < S::BT / 64)
-            to_lds4(xs + b * xs_step, buf + S::kLines * kBlock + wave * 256);
-    };
+            load(i, w, x, 0, lds);
+        load_scales(make_rsrc(from.xs, from.xs_bytes), 0, lds);
+    }
     // this lane's place in a piece of 16 lines: line lane % 16, 16-byte piece lane / 16 (and 4 further)
     const int at = (lane & 15) * kBlock + (((lane >> 4) ^ ((lane & 15) >> 1)) * 16);
-    stage(0, lds);
+    auto fragment = [&](const unsigned char *p) {
+        return join(*reinterpret_cast<const u4 *>(p + at), *reinterpret_cast<const u4 *>(p + (at ^ 64)));
+    };
+    float sw0 = uniform_load(ws0), sw1 = HALVES ? uniform_load(ws1) : 0.0f;
     __syncthreads();
     for (int32_t b = 0; b < kb; ++b) {
         const unsigned char *buf = lds + (b & 1) * S::kStage;
-        if (b + 1 < kb)
-            stage(b + 1, lds + (b + 1 & 1) * S::kStage);
+        unsigned char *other = lds + (b + 1 & 1) * S::kStage;
+        // past the last block the loads are out of their range and read nothing
+        const bool more = b + 1 < kb;
+        const Rsrc w = make_rsrc(from.w, more ? from.w_bytes : 0), x = make_rsrc(from.x, more ? from.x_bytes : 0);
+        const Rsrc xs = make_rsrc(from.xs, more ? from.xs_bytes : 0);
         const unsigned char *wl = buf + wc * S::NC * 16 * kBlock;
         const unsigned char *xl = buf + (S::BC + wt * S::NT * 16) * kBlock;
         const float *sl = reinterpret_cast<const float *>(buf + S::kLines * kBlock) + wt * S::NT * 16 + (lane & 15);
-        const float sw0 = ws0[b], sw1 = HALVES ? ws1[b] : 0.0f;
+        i8 code = fragment(wl);
         decltype(operand<EXACT>(i8{})) xf[S::NT];
         float s0[S::NT], s1[S::NT];
 #pragma unroll
-        for (int t = 0; t < S::NT; ++t) {
-            xf[t] = operand<EXACT>(join(*reinterpret_cast<const u4 *>(xl + t * 16 * kBlock + at),
-                                        *reinterpret_cast<const u4 *>(xl + t * 16 * kBlock + (at ^ 64))));
-            s0[t] = sl[t * 16] * sw0;
-            s1[t] = sl[t * 16] * sw1;
-        }
+        for (int t = 0; t < S::NT; ++t)
+            xf[t] = operand<EXACT>(fragment(xl + t * 16 * kBlock));
+#pragma unroll
+        for (int t = 0; t < S::NT; ++t)
+            s0[t] = sl[t * 16];
+        __builtin_amdgcn_sched_barrier(0);
+        f4 p[2][S::NT];
+        auto add = [&](int c, int t) {
+            const float s = HALVES && c >= S::NC / 2 ? s1[t] : s0[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                acc[c][t][i] = fmaf(s, p[c & 1][t][i], acc[c][t][i]);
+            asm volatile("" : "+v"(acc[c][t]));
+        };
 #pragma unroll
         for (int c = 0; c < S::NC; ++c) {
-            const auto wf = operand<EXACT>(join(*reinterpret_cast<const u4 *>(wl + c * 16 * kBlock + at),
-                                                *reinterpret_cast<const u4 *>(wl + c * 16 * kBlock + (at ^ 64))));
+            const auto wf = operand<EXACT>(code);
+            if (c + 1 < S::NC)
+                code = fragment(wl + (c + 1) * 16 * kBlock);
 #pragma unroll
             for (int t = 0; t < S::NT; ++t) {
-                const f4 p = mfma128(wf, xf[t]);
-                const float s = HALVES && c >= S::NC / 2 ? s1[t] : s0[t];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc[c][t][i] = fmaf(s, p[i], acc[c][t][i]);
+                p[c & 1][t] = mfma128(wf, xf[t]);
+                if (c == 0) {
+                    s1[t] = HALVES ? s0[t] * sw1 : 0.0f;
+                    s0[t] *= sw0;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int kStep = S::kStep;
+                const int id = c * S::NT + t;
+                if (id % kStep == kStep - 1 && id / kStep < S::kLoads)
+                    load(id / kStep, w, x, b + 1, other);
+                if (id == kStep * S::kLoads - 1)
+                    load_scales(xs, b + 1, other);
+                __builtin_amdgcn_sched_barrier(0);
+                if (c > 0)
+                    add(c - 1, t);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+#pragma unroll
+        for (int t = 0; t < S::NT; ++t)
+            add(S::NC - 1, t);
+        // the next block's scales: asked for here, so that no later wait for operands in LDS is one for them
+        sw0 = uniform_load(ws0 + min(b + 1, kb - 1));
+        sw1 = HALVES ? uniform_load(ws1 + min(b + 1, kb - 1)) : 0.0f;
         __syncthreads();
     }
 }
