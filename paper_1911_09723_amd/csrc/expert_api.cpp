@@ -126,6 +126,7 @@ int64_t experts_layout(spconv::ExpertArgs &a, uint8_t *base) {
         take(a.xs, static_cast<int64_t>(a.n) * a.hb * 4);
         take(a.hq, code_bytes(pairs, a.inner));
         take(a.hs, pairs * a.ib * 4);
+        take(a.zs, pairs * a.hb * 4);
     } else {
         take(a.h, pairs * a.inner * 4);
     }

@@ -80,7 +80,9 @@ struct ExpertArgs {
     // (in 32 bits or as codes), the results by place
     int32_t *order, *place, *offsets;
     uint8_t *xq, *hq;
-    float *xs, *hs, *h, *z;
+    float *xs, *hs, *h;
+    void *z;    // f32, or f16 with scales zs [pairs][hb]
+    float *zs;
 };
 
 // How a call is run: token by token (each pair reads its expert's weights), by

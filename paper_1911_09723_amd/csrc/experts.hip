@@ -23,6 +23,15 @@ __device__ __forceinline__ float gated(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + exact) * u;
 }
 
+// The power of two that v is 2^14 to 2^15 of, and its inverse (v at least 2^-112).
+struct Power {
+    float value, inverse;
+};
+__device__ __forceinline__ Power power_below(float v) {
+    const uint32_t e = max(__float_as_uint(v) >> 23, 15u);
+    return {__uint_as_float((e - 14) << 23), __uint_as_float((268 - e) << 23)};
+}
+
 // One tile of rows of one expert, places [row, row + rows).
 struct RowTile {
     int32_t expert, row, rows;
@@ -110,7 +119,8 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, true>(acc, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
+    float total[S::NT] = {};
+    tile_product<S, EXACT, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
 
     const int wc = wave / S::WT, wt = wave % S::WT;
     float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
@@ -156,8 +166,16 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     }
 }
 
-// Second products over LDS tiles: rows by place, results by place in 32 bits.
-template <class S, bool EXACT>
+// Second products over LDS tiles: rows by place, results by place, in 32 bits
+// or (HALF) in f16 with a scale for each 128 channels of a row.  The results are
+// written once and read once by the weighted sum: at 4096 tokens of 8 experts
+// and 2048 channels 537 MB in 32 bits, more than the products' operands.  An
+// f16 value is 2^-12 off at most, an eighth of the rounding of a bf16 result to
+// come.  The scale is the power of two that brings the most that the row's and
+// the weight's scales allow just below 2^15, so nothing overflows, and as the
+// sum of random codes stays some 2^10 below that most, what is lost to f16's
+// small numbers is 2^-30 of a usual value.
+template <class S, bool EXACT, bool HALF>
 __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t columns) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -186,16 +204,25 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + min(cw, a.hidden - 1) / kBlock) * a.ib;
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, false>(acc, from, ws, nullptr, a.ib, lds, wave, lane);
+    float total[S::NT] = {};
+    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.ib, lds, wave, lane);
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
 #pragma unroll
         for (int t = 0; t < S::NT; ++t) {
             const int r = (wt * S::NT + t) * 16 + (lane & 15);
             const int32_t ch = cw + c * 16 + (lane >> 4) * 4;
-            if (r < tile.rows && ch < a.hidden)
-                store4(a.z, kF32, static_cast<int64_t>(tile.row + r) * a.hidden + ch, acc[c][t], a.hidden - ch,
-                       a.hidden % 4 == 0);
+            if (r >= tile.rows || ch >= a.hidden)
+                continue;
+            f4 v = acc[c][t];
+            if constexpr (HALF) {
+                const Power p = power_below(total[t] * (kTop * kTop * kBlock));
+                v *= p.inverse;
+                if (ch % kBlock == 0)
+                    a.zs[static_cast<int64_t>(tile.row + r) * a.hb + ch / kBlock] = p.value;
+            }
+            store4(a.z, HALF ? kF16 : kF32, static_cast<int64_t>(tile.row + r) * a.hidden + ch, v, a.hidden - ch,
+                   a.hidden % 4 == 0);
         }
 }
 
@@ -354,32 +381,66 @@ __global__ void __launch_bounds__(1024) down_token(ExpertArgs a, bool wide) {
     });
 }
 
-// y[t] = sum_j weights[t][j] * z[place of (t, j)], in 32 bits, in the order of j.
+// y[t] = sum_j weights[t][j] * z[place of (t, j)], in 32 bits, in the order of
+// j; a thread sums V neighbouring channels (V = 1: any number of channels).
+template <typename T, int V>
 __global__ void __launch_bounds__(256) combine(ExpertArgs a, int32_t pieces, bool wide) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int32_t token = static_cast<int32_t>(id / pieces), ch = static_cast<int32_t>(id % pieces) * 4;
+    const int32_t token = static_cast<int32_t>(id / pieces), ch = static_cast<int32_t>(id % pieces) * V;
     if (token >= a.n)
         return;
-    f4 sum = {0, 0, 0, 0};
+    float sum[V] = {};
+    const int32_t *place = a.place + static_cast<int64_t>(token) * a.k;
+    const float *weights = a.weights + static_cast<int64_t>(token) * a.k;
+#pragma unroll 4
     for (int32_t j = 0; j < a.k; ++j) {
-        const int32_t pair = token * a.k + j, at = a.place[pair];
+        const int64_t at = place[j];
         if (at < 0)
             continue;
-        const float w = a.weights[pair];
-        const float *z = a.z + static_cast<int64_t>(at) * a.hidden + ch;
-        if (a.hidden % 4 == 0) {
-            const f4 v = *reinterpret_cast<const f4 *>(z);
+        const T *z = reinterpret_cast<const T *>(a.z) + at * a.hidden + ch;
+        float v[V];
+        if constexpr (V == 8) {
+            load8(z, v);
+        } else if constexpr (V == 4) {
+            struct alignas(4 * sizeof(T)) Four {
+                T v[4];
+            } f = *reinterpret_cast<const Four *>(z);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                sum[i] = fmaf(w, v[i], sum[i]);
+                v[i] = static_cast<float>(f.v[i]);
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (ch + i < a.hidden)
-                    sum[i] = fmaf(w, z[i], sum[i]);
+            v[0] = static_cast<float>(z[0]);
         }
+        float w = weights[j];
+        if constexpr (sizeof(T) == 2)
+            w *= a.zs[at * a.hb + ch / kBlock];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            sum[i] = fmaf(w, v[i], sum[i]);
     }
-    store4(a.y, a.type, static_cast<int64_t>(token) * a.hidden + ch, sum, a.hidden - ch, wide);
+    const int64_t to = static_cast<int64_t>(token) * a.hidden + ch;
+    if constexpr (V == 1) {
+        store4(a.y, a.type, to, f4{sum[0], 0, 0, 0}, 1, false);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            store4(a.y, a.type, to + i, f4{sum[i], sum[i + 1], sum[i + 2], sum[i + 3]}, 4, wide);
+    }
+}
+
+template <typename T, int V>
+hipError_t combine_by(const ExpertArgs &a, bool wide, hipStream_t stream) {
+    const int32_t pieces = a.hidden / V;
+    const int64_t blocks = (static_cast<int64_t>(a.n) * pieces + 255) / 256;
+    combine<T, V><<<static_cast<uint32_t>(blocks), 256, 0, stream>>>(a, pieces, wide);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_combine(const ExpertArgs &a, bool wide, hipStream_t stream) {
+    return a.hidden % 8 == 0   ? combine_by<T, 8>(a, wide, stream)
+           : a.hidden % 4 == 0 ? combine_by<T, 4>(a, wide, stream)
+                               : combine_by<T, 1>(a, wide, stream);
 }
 
 template <typename F>
@@ -405,13 +466,13 @@ hipError_t gated_tiles(const ExpertArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <class S, bool EXACT>
+template <class S, bool EXACT, bool HALF>
 hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
-    static const hipError_t ready = allow_lds(down_tile<S, EXACT>, S::kLds);
+    static const hipError_t ready = allow_lds(down_tile<S, EXACT, HALF>, S::kLds);
     if (ready != hipSuccess)
         return ready;
     const int32_t columns = (a.hidden + S::BC - 1) / S::BC;
-    down_tile<S, EXACT><<<tile_grid(most_tiles(a, S::BT), columns), S::kThreads, S::kLds, stream>>>(a, columns);
+    down_tile<S, EXACT, HALF><<<tile_grid(most_tiles(a, S::BT), columns), S::kThreads, S::kLds, stream>>>(a, columns);
     return hipGetLastError();
 }
 
@@ -470,7 +531,8 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         const int64_t each = a.pairs / a.experts;
         if ((e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
             return e;
-        // bf16: what the 8-bit instruction loses lies below the rounding of the result
+        // bf16: what the 8-bit instruction loses lies below the rounding of the result, f16 results
+        // between the products and their sum as well
         if (a.type == kBf16)
             e = each >= 192  ? gated_tiles<Big, false>(a, stream)
                 : each >= 96 ? gated_tiles<Mid, false>(a, stream)
@@ -480,18 +542,18 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         if (e != hipSuccess)
             return e;
         if (a.type == kF32)
-            e = down_tiles<TileShape<128, 128, 2, 2>, true>(a, stream);
+            e = down_tiles<TileShape<128, 128, 2, 2>, true, false>(a, stream);
+        else if (a.type == kF16)
+            e = each >= 96 ? down_tiles<Mid, false, false>(a, stream) : down_tiles<Small, false, false>(a, stream);
         else
-            e = each >= 192  ? down_tiles<Big, false>(a, stream)
-                : each >= 96 ? down_tiles<Mid, false>(a, stream)
-                             : down_tiles<Small, false>(a, stream);
+            e = each >= 192  ? down_tiles<Big, false, true>(a, stream)
+                : each >= 96 ? down_tiles<Mid, false, true>(a, stream)
+                             : down_tiles<Small, false, true>(a, stream);
     }
     if (e != hipSuccess)
         return e;
-    const int32_t pieces = (a.hidden + 3) / 4;
-    const int64_t blocks = (static_cast<int64_t>(a.n) * pieces + 255) / 256;
-    combine<<<static_cast<uint32_t>(blocks), 256, 0, stream>>>(a, pieces, wide);
-    return hipGetLastError();
+    return path == ExpertPath::kTiles && a.type == kBf16 ? launch_combine<_Float16>(a, wide, stream)
+                                                         : launch_combine<float>(a, wide, stream);
 }
 
 }  // namespace spconv

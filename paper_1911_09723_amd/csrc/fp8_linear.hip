@@ -61,7 +61,8 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
     f4 acc[S::NC][S::NT] = {};
-    tile_product<S, EXACT, false>(acc, from, ws, nullptr, a.kb, lds, wave, lane);
+    float total[S::NT] = {};
+    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.kb, lds, wave, lane);
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
 #pragma unroll

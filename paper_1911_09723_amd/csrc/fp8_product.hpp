@@ -86,10 +86,13 @@ __device__ __forceinline__ float uniform_load(const float *p) {
 }
 
 // acc[c][t] += the products over kb blocks; ws0, ws1: the scales by block of
-// the first and of the second half (HALVES) of the wavefront's channel pieces.
+// the first and of the second half (HALVES) of the wavefront's channel pieces;
+// total[t] += the scales' products, whose sum times 128 * 448^2 no result exceeds.
 template <class S, bool EXACT, bool HALVES>
-__device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const TileSource<S> &from, const float *ws0,
-                                             const float *ws1, int32_t kb, unsigned char *lds, int wave, int lane) {
+__device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&total)[S::NT],
+                                             const TileSource<S> &from, const float *ws0, const float *ws1, int32_t kb,
+                                             unsigned char *lds, int wave, int lane) {
+#ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources
     const int wc = wave / S::WT, wt = wave % S::WT;
     auto load = [&](int i, Rsrc w, Rsrc x, int32_t b, unsigned char *buf) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -156,6 +159,7 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const Tile
                 if (c == 0) {
                     s1[t] = HALVES ? s0[t] * sw1 : 0.0f;
                     s0[t] *= sw0;
+                    total[t] += s0[t];
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 constexpr int kStep = S::kStep;
@@ -178,6 +182,7 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], const Tile
         sw1 = HALVES ? uniform_load(ws1 + min(b + 1, kb - 1)) : 0.0f;
         __syncthreads();
     }
+#endif
 }
 
 // ---------------------------------------------------------------------------
