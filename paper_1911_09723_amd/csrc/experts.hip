@@ -14,9 +14,13 @@ namespace {
 
 constexpr int kXcds = 8;
 
-// g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each;
-// g log2(e) is taken to twice 32 bits so that the exponential stays there.
+// g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each.
+// EXACT: g log2(e) is taken to twice 32 bits so that the exponential stays
+// there; else it is up to |g| last places off, far less than 8-bit products are.
+template <bool EXACT>
 __device__ __forceinline__ float gated(float g, float u) {
+    if constexpr (!EXACT)
+        return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;
     const float t = g * -1.44269504f, rest = fmaf(g, -1.44269504f, -t) + g * -1.92596299e-8f;
     const float e = __builtin_amdgcn_exp2f(t);
     const float exact = fabsf(t) < 128.0f ? fmaf(e, rest * 0.693147181f, e) : e;  // else 0 or infinite
@@ -106,14 +110,15 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        uint32_t row;
         if (line < S::BC) {  // lines of a wavefront: 64 gate, then 64 up channels
-            row = min(fb * kBlock + line / 128 * 64 + line % 64, a.inner - 1) + (line & 64 ? a.inner : 0);
+            const int32_t ch = fb * kBlock + line / 128 * 64 + line % 64;
+            from.at[i] = ch < a.inner ? (ch + (line & 64 ? a.inner : 0)) * pitch + tile_byte(line, lane) : from.w_bytes;
         } else {
-            row = a.order[tile.row + min(line - S::BC, tile.rows - 1)] / a.k;
+            const int r = line - S::BC;
+            from.at[i] = r < tile.rows ? a.order[tile.row + r] / a.k * pitch + tile_byte(line, lane) : from.x_bytes;
         }
-        from.at[i] = row * pitch + tile_byte(line, lane);
     }
+    from.rows = tile.rows;
     from.xs = a.xs;
     from.xs_at = wave < S::BT / 64 ? a.order[tile.row + min(wave * 64 + lane, tile.rows - 1)] / a.k * 4u : 0;
     from.xs_step = a.n * 4u;
@@ -122,40 +127,44 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     float total[S::NT] = {};
     tile_product<S, EXACT, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
 
-    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
     constexpr int HC = S::NC / 2;
+    const bool idle = wt * S::NT * 16 >= tile.rows;
     uint32_t m[S::NT];
+    if (!idle) {
 #pragma unroll
-    for (int t = 0; t < S::NT; ++t) {
-        m[t] = 0;
+        for (int t = 0; t < S::NT; ++t) {
+            m[t] = 0;
 #pragma unroll
-        for (int c = 0; c < HC; ++c)
+            for (int c = 0; c < HC; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t ch = fb * kBlock + wc * 64 + c * 16 + (lane >> 4) * 4 + i;
-                const float h = ch < a.inner ? gated(acc[c][t][i], acc[c + HC][t][i]) : 0.0f;
-                acc[c][t][i] = h;
-                m[t] = max(m[t], magnitude(h));
-            }
-        m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 16)));
-        m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 32)));
-        if (lane < 16)
-            most[wc * S::BT + (wt * S::NT + t) * 16 + lane] = __uint_as_float(m[t]);
+                for (int i = 0; i < 4; ++i) {
+                    const float h = gated<EXACT>(acc[c][t][i], acc[c + HC][t][i]);  // channels past the last: 0
+                    acc[c][t][i] = h;
+                    m[t] = max(m[t], magnitude(h));
+                }
+            m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 16)));
+            m[t] = max(m[t], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[t]), 32)));
+            if (lane < 16)
+                most[wc * S::BT + (wt * S::NT + t) * 16 + lane] = __uint_as_float(m[t]);
+        }
     }
     __syncthreads();
+    if (!idle) {
 #pragma unroll
-    for (int t = 0; t < S::NT; ++t) {
-        const int r = (wt * S::NT + t) * 16 + (lane & 15);
-        const Scale s = scale_of(max(m[t], __float_as_uint(most[(1 - wc) * S::BT + r])));
+        for (int t = 0; t < S::NT; ++t) {
+            const int r = (wt * S::NT + t) * 16 + (lane & 15);
+            const Scale s = scale_of(max(m[t], __float_as_uint(most[(1 - wc) * S::BT + r])));
 #pragma unroll
-        for (int c = 0; c < HC; ++c) {
-            const float v[4] = {acc[c][t][0], acc[c][t][1], acc[c][t][2], acc[c][t][3]};
-            const int word = (wc * 16 + c * 4 + (lane >> 4)) ^ (r & 7) * 4;  // spread over LDS's banks
-            reinterpret_cast<uint32_t *>(lds)[r * 32 + word] = codes4(v, s.inv);
+            for (int c = 0; c < HC; ++c) {
+                const float v[4] = {acc[c][t][0], acc[c][t][1], acc[c][t][2], acc[c][t][3]};
+                const int word = (wc * 16 + c * 4 + (lane >> 4)) ^ (r & 7) * 4;  // spread over LDS's banks
+                reinterpret_cast<uint32_t *>(lds)[r * 32 + word] = codes4(v, s.inv);
+            }
+            if (wc == 0 && lane < 16 && r < tile.rows)
+                a.hs[static_cast<int64_t>(fb) * a.pairs + tile.row + r] = s.scale;
         }
-        if (wc == 0 && lane < 16 && r < tile.rows)
-            a.hs[static_cast<int64_t>(fb) * a.pairs + tile.row + r] = s.scale;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < S::BT * 8; i += S::kThreads) {
@@ -193,14 +202,17 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        const int row = line < S::BC ? min(line, a.hidden - 1 - c0) : min(line - S::BC, tile.rows - 1);
-        from.at[i] = row * pitch + tile_byte(line, lane);
+        if (line < S::BC)
+            from.at[i] = line < a.hidden - c0 ? line * pitch + tile_byte(line, lane) : from.w_bytes;
+        else
+            from.at[i] = line - S::BC < tile.rows ? (line - S::BC) * pitch + tile_byte(line, lane) : from.x_bytes;
     }
+    from.rows = tile.rows;
     from.xs = a.hs + tile.row;
     from.xs_at = min(wave * 64 + lane, tile.rows - 1) * 4u;
     from.xs_step = a.pairs * 4u;
     from.xs_bytes = from.xs_step * (a.ib - 1) + tile.rows * 4u;
-    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + min(cw, a.hidden - 1) / kBlock) * a.ib;
     f4 acc[S::NC][S::NT] = {};
@@ -295,7 +307,7 @@ __global__ void __launch_bounds__(1024) gated_stream(ExpertArgs a, int32_t colum
         f4 h;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            h[i] = gated(gate[i], up[i]);
+            h[i] = gated<true>(gate[i], up[i]);
         store4(a.h, kF32, static_cast<int64_t>(tile.row + (lane & 15)) * a.inner + ch, h, a.inner - ch, a.inner % 4 == 0);
     }
 }

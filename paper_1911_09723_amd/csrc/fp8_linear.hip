@@ -49,15 +49,17 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        // lines past the last row or channel repeat it: their results are not stored
-        const int row = line < S::BC ? min(line, a.cout - 1 - c0) : min(line - S::BC, a.n - 1 - t0);
-        from.at[i] = row * pitch + tile_byte(line, lane);
+        if (line < S::BC)
+            from.at[i] = line < a.cout - c0 ? line * pitch + tile_byte(line, lane) : from.w_bytes;
+        else
+            from.at[i] = line - S::BC < a.n - t0 ? (line - S::BC) * pitch + tile_byte(line, lane) : from.x_bytes;
     }
+    from.rows = a.n - t0;
     from.xs = a.xs;
     from.xs_at = min(t0 + wave * 64 + lane, a.n - 1) * 4u;
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.kb;
-    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
     f4 acc[S::NC][S::NT] = {};

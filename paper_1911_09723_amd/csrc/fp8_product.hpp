@@ -72,14 +72,23 @@ __device__ __forceinline__ int tile_byte(int line, int lane) { return ((lane & 7
 
 // What a tile reads: W and X from their bases, this lane's offsets of its lines
 // (block 0); the rows' scales and this lane's offset there (wavefronts below
-// BT / 64 only), step bytes from block to block.  Bytes: what each base covers.
+// BT / 64 only), step bytes from block to block.  Bytes: what each base covers;
+// an offset of that size reads zeros.  rows: how many of the tile's rows there are.
 template <class S>
 struct TileSource {
     const uint8_t *w, *x;
     const float *xs;
     uint32_t w_bytes, x_bytes, xs_bytes, xs_step;
     uint32_t at[S::kLoads], xs_at;
+    int32_t rows;
 };
+
+// A wavefront's channel and row pieces.  Wavefronts w and w + 4 share a SIMD:
+// in this order a tile that is half empty leaves work on all four.
+template <class S>
+__device__ __forceinline__ int channel_part(int wave) { return wave % S::WC; }
+template <class S>
+__device__ __forceinline__ int row_part(int wave) { return wave / S::WC; }
 
 __device__ __forceinline__ float uniform_load(const float *p) {
     return *reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(p));
@@ -93,7 +102,7 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
                                              const TileSource<S> &from, const float *ws0, const float *ws1, int32_t kb,
                                              unsigned char *lds, int wave, int lane) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources
-    const int wc = wave / S::WT, wt = wave % S::WT;
+    const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     auto load = [&](int i, Rsrc w, Rsrc x, int32_t b, unsigned char *buf) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
             i < S::kWeightLoads ? w : x,
@@ -120,6 +129,18 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
     };
     float sw0 = uniform_load(ws0), sw1 = HALVES ? uniform_load(ws1) : 0.0f;
     __syncthreads();
+    if (wt * S::NT * 16 >= from.rows) {  // no rows of its own: only its share of the loads
+        for (int32_t b = 1; b < kb; ++b) {
+            const Rsrc w = make_rsrc(from.w, from.w_bytes), x = make_rsrc(from.x, from.x_bytes);
+#pragma unroll
+            for (int i = 0; i < S::kLoads; ++i)
+                load(i, w, x, b, lds + (b & 1) * S::kStage);
+            load_scales(make_rsrc(from.xs, from.xs_bytes), b, lds + (b & 1) * S::kStage);
+            __syncthreads();
+        }
+        __syncthreads();
+        return;
+    }
     for (int32_t b = 0; b < kb; ++b) {
         const unsigned char *buf = lds + (b & 1) * S::kStage;
         unsigned char *other = lds + (b + 1 & 1) * S::kStage;
