@@ -218,24 +218,21 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
     tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.ib, lds, wave, lane);
-#pragma unroll
-    for (int c = 0; c < S::NC; ++c)
+    const int32_t ch = cw + (lane >> 4) * 4;
+    float inverse[S::NT];
+    if constexpr (HALF) {
+        static_assert(S::NC * 16 == kBlock, "a wavefront's channels are one block");
 #pragma unroll
         for (int t = 0; t < S::NT; ++t) {
             const int r = (wt * S::NT + t) * 16 + (lane & 15);
-            const int32_t ch = cw + c * 16 + (lane >> 4) * 4;
-            if (r >= tile.rows || ch >= a.hidden)
-                continue;
-            f4 v = acc[c][t];
-            if constexpr (HALF) {
-                const Power p = power_below(total[t] * (kTop * kTop * kBlock));
-                v *= p.inverse;
-                if (ch % kBlock == 0)
-                    a.zs[static_cast<int64_t>(tile.row + r) * a.hb + ch / kBlock] = p.value;
-            }
-            store4(a.z, HALF ? kF16 : kF32, static_cast<int64_t>(tile.row + r) * a.hidden + ch, v, a.hidden - ch,
-                   a.hidden % 4 == 0);
+            const Power p = power_below(total[t] * (kTop * kTop * kBlock));
+            inverse[t] = p.inverse;
+            if (lane < 16 && r < tile.rows && cw < a.hidden)
+                a.zs[static_cast<int64_t>(tile.row + r) * a.hb + cw / kBlock] = p.value;
         }
+    }
+    store_tile<S>(acc, a.z, HALF ? kF16 : kF32, tile.row, tile.rows, ch, a.hidden, a.hidden % 4 == 0, wt, lane,
+                  [&](f4 v, int, int t) { return HALF ? v * inverse[t] : v; });
 }
 
 // First products of a few rows: 16 gate and 16 up channels of up to 16 rows, which are

@@ -174,6 +174,17 @@ __device__ __forceinline__ float clamp_to(float v, float lo, float hi) {
     return v > hi ? hi : v;
 }
 
+// Four values rounded once to f16 or bf16.
+template <int TYPE>
+__device__ __forceinline__ u2 rounded4(f4 v) {
+    uint16_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        r[i] = TYPE == kF16 ? __builtin_bit_cast(uint16_t, static_cast<_Float16>(v[i]))
+                            : __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[i]));
+    return u2{r[0] | static_cast<uint32_t>(r[1]) << 16, r[2] | static_cast<uint32_t>(r[3]) << 16};
+}
+
 // `left` (1 to 4) neighbouring values to y + at, rounded once to its type; `wide`:
 // the four start on a multiple of their size.
 __device__ __forceinline__ void store4(void *y, int32_t type, int64_t at, f4 v, int left, bool wide) {
@@ -189,20 +200,16 @@ __device__ __forceinline__ void store4(void *y, int32_t type, int64_t at, f4 v, 
                 p[i] = v[i];
         return;
     }
-    uint16_t r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        r[i] = type == kF16 ? __builtin_bit_cast(uint16_t, static_cast<_Float16>(v[i]))
-                            : __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[i]));
+    const u2 r = type == kF16 ? rounded4<kF16>(v) : rounded4<kBf16>(v);
     uint16_t *p = static_cast<uint16_t *>(y) + at;
     if (wide && left >= 4) {
-        *reinterpret_cast<u2 *>(p) = u2{r[0] | static_cast<uint32_t>(r[1]) << 16, r[2] | static_cast<uint32_t>(r[3]) << 16};
+        *reinterpret_cast<u2 *>(p) = r;
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (i < left)
-            p[i] = r[i];
+            p[i] = static_cast<uint16_t>(r[i >> 1] >> (i & 1) * 16);
 }
 
 }  // namespace spconv

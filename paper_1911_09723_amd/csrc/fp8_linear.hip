@@ -65,11 +65,20 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
     tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.kb, lds, wave, lane);
+    const int32_t ch = cw + (lane >> 4) * 4;
+    f4 bias[S::NC];
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
+        bias[c] = bias4(a.bias, ch + c * 16, a.cout);
+    const bool clamp = a.lo > -INFINITY || a.hi < INFINITY;
+    store_tile<S>(acc, a.y, a.y_type, t0, a.n - t0, ch, a.cout, wide, wt, lane, [&](f4 v, int c, int) {
+        v += bias[c];
+        if (clamp)
 #pragma unroll
-        for (int t = 0; t < S::NT; ++t)
-            finish(a, wide, t0 + (wt * S::NT + t) * 16 + (lane & 15), cw + c * 16 + (lane >> 4) * 4, acc[c][t]);
+            for (int i = 0; i < 4; ++i)
+                v[i] = clamp_to(v[i], a.lo, a.hi);
+        return v;
+    });
 }
 
 // XT: Fp8 (codes) or the type of rows that are quantised here.

@@ -206,6 +206,53 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
 #endif
 }
 
+// A wavefront's results to rows of y: `row` is y's first row of the tile, `rows`
+// how many it has, ch this lane's first channel of piece 0, `channels` y's row.
+// `finish(v, c, t)` gives what is stored for piece (c, t).
+template <class S, int TYPE, class F>
+__device__ __forceinline__ void store_whole(const f4 (&acc)[S::NC][S::NT], void *y, int64_t row, int32_t rows, int32_t ch,
+                                            int32_t channels, int wt, int lane, F finish) {
+    constexpr int kSize = TYPE == kF32 ? 4 : 2;
+#pragma unroll
+    for (int t = 0; t < S::NT; ++t) {
+        const int r = (wt * S::NT + t) * 16 + (lane & 15);
+        if (r >= rows)
+            continue;
+        char *p = static_cast<char *>(y) + ((row + r) * channels + ch) * kSize;
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) {
+            const f4 v = finish(acc[c][t], c, t);
+            if constexpr (TYPE == kF32)
+                *reinterpret_cast<f4 *>(p + c * 16 * kSize) = v;
+            else
+                *reinterpret_cast<u2 *>(p + c * 16 * kSize) = rounded4<TYPE>(v);
+        }
+    }
+}
+
+// The same for any channels and alignment; `wide`: four neighbours may be stored at once.
+template <class S, class F>
+__device__ __forceinline__ void store_tile(const f4 (&acc)[S::NC][S::NT], void *y, int32_t type, int64_t row, int32_t rows,
+                                           int32_t ch, int32_t channels, bool wide, int wt, int lane, F finish) {
+    if (wide && ch - (lane >> 4) * 4 + S::NC * 16 <= channels) {
+        if (type == kF32)
+            store_whole<S, kF32>(acc, y, row, rows, ch, channels, wt, lane, finish);
+        else if (type == kF16)
+            store_whole<S, kF16>(acc, y, row, rows, ch, channels, wt, lane, finish);
+        else
+            store_whole<S, kBf16>(acc, y, row, rows, ch, channels, wt, lane, finish);
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < S::NT; ++t) {
+        const int r = (wt * S::NT + t) * 16 + (lane & 15);
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+            if (r < rows && ch + c * 16 < channels)
+                store4(y, type, (row + r) * channels + ch + c * 16, finish(acc[c][t], c, t), channels - ch - c * 16, wide);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Stream core: up to 16 TT rows against CT pieces of 16 channels, the blocks
 // of the input channels dealt to the wavefronts of a workgroup in turn.
