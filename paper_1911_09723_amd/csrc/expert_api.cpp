@@ -111,7 +111,7 @@ int64_t experts_layout(spconv::ExpertArgs &a, uint8_t *base) {
     int64_t at = 0;
     auto take = [&](auto &p, int64_t bytes) {
         p = base ? reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at) : nullptr;
-        at += align16(bytes);
+        at += (bytes + 255) / 256 * 256;  // codes on whole 128-byte lines: else a product reads two for one
     };
     const int64_t pairs = a.pairs;
     const spconv::ExpertPath path = spconv::expert_path(a.n, a.k, a.experts);
