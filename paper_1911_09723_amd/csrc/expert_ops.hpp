@@ -76,8 +76,8 @@ struct ExpertArgs {
     int32_t type;              // of x and y
     int32_t n, k, pairs, experts, hidden, inner;
     int32_t hb, ib;            // blocks of 128 hidden and inner channels
-    // workspace: the pairs' order by expert, x's codes, the inner rows by place
-    // (in 32 bits or as codes), the results by place
+    // workspace: the pairs' order by expert, x's codes, the inner rows in 32 bits and
+    // as codes, and the results, by place (token by token: by pair)
     int32_t *order, *place, *offsets;
     uint8_t *xq, *hq;
     float *xs, *hs, *h;
@@ -88,7 +88,7 @@ struct ExpertArgs {
 // How a call is run: token by token (each pair reads its expert's weights), by
 // expert with the rows of 16 at a time against streamed weights, or over LDS tiles.
 enum class ExpertPath { kTokens, kFew, kTiles };
-ExpertPath expert_path(int32_t n, int32_t k, int32_t experts);
+ExpertPath expert_path(int32_t n, int32_t k, int32_t experts, int32_t inner);
 hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream);
 
 }  // namespace spconv

@@ -235,37 +235,38 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
                   [&](f4 v, int, int t) { return HALF ? v * inverse[t] : v; });
 }
 
-// First products of a few rows: 16 gate and 16 up channels of up to 16 rows, which are
-// quantised here.  DIRECT: a workgroup's row is pair blockIdx.y itself, unsorted.
-template <typename T, int U, bool DIRECT>
-__global__ void __launch_bounds__(1024) gated_stream(ExpertArgs a, int32_t columns, bool wide) {
+// Few rows.  What bounds them is the weights' bytes, and a compute unit takes in
+// no more than its share of the card's rate (some 20 GB/s: what it can have
+// outstanding, over the memory's latency), so the weights have to be spread
+// evenly over all of them: workgroups of 16 channels (8 for single tokens), the
+// blocks of input channels dealt to their wavefronts.  Workgroups of 128
+// channels, which could convert the inner rows to codes themselves, took 24
+// instead of 14 us for the first products of one token (6 x 4 MB).
+
+// First products of up to 16 rows of one expert, given as codes: 16 gate and 16
+// up channels; the gated result leaves in 32 bits.
+template <int U>
+__global__ void __launch_bounds__(512) gated_rows(ExpertArgs a, int32_t columns) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     RowTile tile;
-    int32_t ct;
-    int32_t token;
-    if constexpr (DIRECT) {
-        tile = RowTile{a.ids[blockIdx.y], static_cast<int32_t>(blockIdx.y), 1};
-        ct = blockIdx.x;
-        if (tile.expert < 0 || tile.expert >= a.experts)
-            return;
-        token = tile.row / a.k;
-    } else {
-        if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &ct))
-            return;
-        token = a.order[tile.row + min(lane & 15, tile.rows - 1)] / a.k;
-    }
-    const int32_t c0 = ct * 16;
+    int32_t column;
+    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &column))
+        return;
+    const int32_t c0 = column * 16;
     const int64_t pitch = static_cast<int64_t>(a.hb) * kBlock;
     const uint8_t *wg = a.w13 + (static_cast<int64_t>(tile.expert) * 2 * a.inner + min(c0 + (lane & 15), a.inner - 1)) * pitch;
     const uint8_t *wu = wg + a.inner * pitch;
     const float *sg = a.s13 + (static_cast<int64_t>(tile.expert) * 2 * a.ib + c0 / kBlock) * a.hb;
     const float *su = sg + static_cast<int64_t>(a.ib) * a.hb;
-    const T *x = static_cast<const T *>(a.x) + token * a.ldx;
+    const int32_t token = a.order[tile.row + min(lane & 15, tile.rows - 1)] / a.k;
+    const uint8_t *x = a.xq + token * pitch;
+    const float *xs = a.xs + token;
     f4 acc[2] = {};
     for (int32_t b0 = wave; b0 < a.hb; b0 += waves * U) {
         i8 g[U], up[U];
+        RowPart xp[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t b = min(b0 + u * waves, a.hb - 1);
@@ -274,13 +275,17 @@ __global__ void __launch_bounds__(1024) gated_stream(ExpertArgs a, int32_t colum
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.hb - 1);
+            xp[u] = row_codes(x, xs + static_cast<int64_t>(b) * a.n, b, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
             const int32_t b = b0 + u * waves;
             if (b >= a.hb)
                 break;
-            const RowPart xp = row_quantized(x, b, a.hidden, wide, lane);
-            const Halves xh = halves(xp.code);
+            const Halves xh = halves(xp[u].code);
             const f4 p = mfma128(halves(g[u]), xh), q = mfma128(halves(up[u]), xh);
-            const float s0 = xp.scale * sg[b], s1 = xp.scale * su[b];
+            const float s0 = xp[u].scale * uniform_load(sg + b), s1 = xp[u].scale * uniform_load(su + b);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 acc[0][i] = fmaf(s0, p[i], acc[0][i]);
@@ -309,85 +314,220 @@ __global__ void __launch_bounds__(1024) gated_stream(ExpertArgs a, int32_t colum
     }
 }
 
-// Second products of a few rows, quantised here; results by place in 32 bits.
-template <int CT, int U>
-__global__ void __launch_bounds__(1024) down_stream(ExpertArgs a, int32_t columns) {
+// Second products of up to 16 rows of one expert, given as codes: 16 channels;
+// results by place in 32 bits.
+template <int U>
+__global__ void __launch_bounds__(512) down_rows(ExpertArgs a, int32_t columns) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     RowTile tile;
-    int32_t ct;
-    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &ct))
+    int32_t column;
+    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &column))
         return;
-    const int32_t c0 = ct * 16 * CT;
+    const int32_t c0 = column * 16;
     const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
-    const uint8_t *w[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-        w[c] = a.w2 + (static_cast<int64_t>(tile.expert) * a.hidden + min(c0 + c * 16 + (lane & 15), a.hidden - 1)) * pitch;
+    const uint8_t *w = a.w2 + (static_cast<int64_t>(tile.expert) * a.hidden + min(c0 + (lane & 15), a.hidden - 1)) * pitch;
     const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + c0 / kBlock) * a.ib;
-    const float *h = a.h + static_cast<int64_t>(tile.row + min(lane & 15, tile.rows - 1)) * a.inner;
-    f4 acc[CT] = {};
+    const int32_t place = tile.row + min(lane & 15, tile.rows - 1);
+    f4 acc[1] = {};
     for (int32_t b0 = wave; b0 < a.ib; b0 += waves * U) {
-        i8 wf[U][CT];
+        i8 wf[U];
+        RowPart xp[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                wf[u][c] = weight_part(w[c], min(b0 + u * waves, a.ib - 1), lane);
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.ib - 1);
+            wf[u] = weight_part(w, b, lane);
+            xp[u] = row_codes(a.hq + place * pitch, a.hs + static_cast<int64_t>(b) * a.pairs + place, b, lane);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t b = b0 + u * waves;
             if (b >= a.ib)
                 break;
-            const RowPart xp = row_quantized(h, b, a.inner, a.inner % 4 == 0, lane);
-            const Halves xh = halves(xp.code);
-            const float s = xp.scale * ws[b];
+            const f4 p = mfma128(halves(wf[u]), halves(xp[u].code));
+            const float s = xp[u].scale * uniform_load(ws + b);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const f4 p = mfma128(halves(wf[u][c]), xh);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc[c][i] = fmaf(s, p[i], acc[c][i]);
-            }
+            for (int i = 0; i < 4; ++i)
+                acc[0][i] = fmaf(s, p[i], acc[0][i]);
         }
-    }
-    sum_waves<CT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int c, f4 sum) {
-        const int32_t ch = c0 + c * 16 + (lane >> 4) * 4;
-        if ((lane & 15) < tile.rows && ch < a.hidden)
-            store4(a.z, kF32, static_cast<int64_t>(tile.row + (lane & 15)) * a.hidden + ch, sum, a.hidden - ch,
-                   a.hidden % 4 == 0);
-    });
-}
-
-// Second products and weighted sum of one token (blockIdx.y): the pairs' blocks
-// of inner channels are one long axis, dealt to the wavefronts in turn.
-__global__ void __launch_bounds__(1024) down_token(ExpertArgs a, bool wide) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int waves = blockDim.x >> 6;
-    const int32_t c0 = blockIdx.x * 16, token = blockIdx.y;
-    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
-    f4 acc[1] = {};
-    for (int32_t item = wave; item < a.k * a.ib; item += waves) {
-        const int32_t j = item / a.ib, b = item - j * a.ib, pair = token * a.k + j;
-        const int32_t e = a.ids[pair];
-        if (e < 0 || e >= a.experts)
-            continue;
-        const int64_t row = static_cast<int64_t>(e) * a.hidden + min(c0 + (lane & 15), a.hidden - 1);
-        const i8 wf = weight_part(a.w2 + row * pitch, b, lane);
-        const RowPart xp = row_quantized(a.h + static_cast<int64_t>(pair) * a.inner, b, a.inner, a.inner % 4 == 0, lane);
-        const f4 p = mfma128(halves(wf), halves(xp.code));
-        const float s = xp.scale * a.s2[(static_cast<int64_t>(e) * a.hb + c0 / kBlock) * a.ib + b] * a.weights[pair];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            acc[0][i] = fmaf(s, p[i], acc[0][i]);
     }
     sum_waves<1>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int, f4 sum) {
         const int32_t ch = c0 + (lane >> 4) * 4;
-        if ((lane & 15) == 0 && ch < a.hidden)
-            store4(a.y, a.type, static_cast<int64_t>(token) * a.hidden + ch, sum, a.hidden - ch, wide);
+        if ((lane & 15) < tile.rows && ch < a.hidden)
+            store4(a.z, kF32, static_cast<int64_t>(place) * a.hidden + ch, sum, a.hidden - ch, a.hidden % 4 == 0);
     });
+}
+
+// Single tokens: one row of x has no use for matrix instructions, and whole rows
+// of W are read in whole lines: a lane takes 16 of 1024 neighbouring channels, 8
+// lanes a block.
+
+// The sum of 16 products of codes.
+__device__ __forceinline__ float dot16(const float *x, u4 w) {
+    float even = 0.0f, odd = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[i]), false);
+        const f2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[i]), true);
+        even = fmaf(x[4 * i], lo[0], even);
+        odd = fmaf(x[4 * i + 1], lo[1], odd);
+        even = fmaf(x[4 * i + 2], hi[0], even);
+        odd = fmaf(x[4 * i + 3], hi[1], odd);
+    }
+    return even + odd;
+}
+
+__device__ __forceinline__ void code_values(u4 c, float *v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(c[i]), false);
+        const f2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(c[i]), true);
+        v[4 * i] = lo[0];
+        v[4 * i + 1] = lo[1];
+        v[4 * i + 2] = hi[0];
+        v[4 * i + 3] = hi[1];
+    }
+}
+
+__device__ __forceinline__ float sum_lanes(float v) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+        v += __shfl_xor(v, s);
+    return v;
+}
+
+__device__ __forceinline__ u4 stream16(const uint8_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p)); }
+
+constexpr int kTokenChannels = 2;  // gate and up channels of a wavefront
+
+// First products of pair blockIdx.y; x is quantised here.
+template <typename T>
+__global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t pair = blockIdx.y, e = a.ids[pair];
+    if (e < 0 || e >= a.experts)
+        return;
+    const int32_t c0 = (static_cast<int32_t>(blockIdx.x) * 4 + wave) * kTokenChannels;
+    if (c0 >= a.inner)
+        return;
+    const int32_t pitch = a.hb * kBlock;
+    const T *x = static_cast<const T *>(a.x) + (pair / a.k) * a.ldx;
+    const uint8_t *row[2 * kTokenChannels];
+#pragma unroll
+    for (int i = 0; i < kTokenChannels; ++i) {
+        row[i] = a.w13 + (static_cast<int64_t>(e) * 2 * a.inner + min(c0 + i, a.inner - 1)) * pitch;
+        row[i + kTokenChannels] = row[i] + static_cast<int64_t>(a.inner) * pitch;
+    }
+    const float *sg = a.s13 + (static_cast<int64_t>(e) * 2 * a.ib + c0 / kBlock) * a.hb;
+    const float *su = sg + static_cast<int64_t>(a.ib) * a.hb;
+    float acc[2 * kTokenChannels] = {};
+    constexpr int U = 2;
+    for (int32_t k0 = lane * 16; k0 < pitch; k0 += U * 1024) {
+        u4 w[U][2 * kTokenChannels];
+        float g[U], u[U], v[U][16];
+        // a lane past the last channel repeats the last block's, times 0
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int32_t k = min(k0 + j * 1024, pitch - 16);
+#pragma unroll
+            for (int i = 0; i < 2 * kTokenChannels; ++i)
+                w[j][i] = stream16(row[i] + k);
+            const bool there = k0 + j * 1024 < pitch;
+            g[j] = there ? sg[k / kBlock] : 0.0f;
+            u[j] = there ? su[k / kBlock] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int32_t k = k0 + j * 1024;
+            load8_tail(x + k, k < pitch ? a.hidden - k : 0, wide, v[j]);
+            load8_tail(x + k + 8, k < pitch ? a.hidden - k - 8 : 0, wide, v[j] + 8);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            uint32_t m = max(most8(v[j]), most8(v[j] + 8));
+#pragma unroll
+            for (int s = 1; s < 8; s *= 2)
+                m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), s)));
+            const Scale s = scale_of(m);
+            const u4 c = {codes4(v[j], s.inv), codes4(v[j] + 4, s.inv), codes4(v[j] + 8, s.inv), codes4(v[j] + 12, s.inv)};
+            code_values(c, v[j]);
+#pragma unroll
+            for (int i = 0; i < kTokenChannels; ++i) {
+                acc[i] = fmaf(dot16(v[j], w[j][i]), s.scale * g[j], acc[i]);
+                acc[i + kTokenChannels] = fmaf(dot16(v[j], w[j][i + kTokenChannels]), s.scale * u[j], acc[i + kTokenChannels]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kTokenChannels; ++i) {
+        const float h = gated<true>(sum_lanes(acc[i]), sum_lanes(acc[i + kTokenChannels]));
+        if (lane == 0 && c0 + i < a.inner)
+            a.h[static_cast<int64_t>(pair) * a.inner + c0 + i] = h;
+    }
+}
+
+// Second products and weighted sum of token blockIdx.y, a channel a wavefront.
+// The workgroup quantises the token's inner rows into LDS while the first
+// weights are on their way.  lds: codes [k][128 ib], scales [k][ib].
+__global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t token = blockIdx.y, ch = min(static_cast<int32_t>(blockIdx.x) * 8 + wave, a.hidden - 1);
+    const int32_t pitch = a.ib * kBlock, chunks = (pitch + 1023) / 1024, items = a.k * chunks;
+    const int32_t *ids = a.ids + token * a.k;
+    const float *weights = a.weights + token * a.k;
+    float *scales = reinterpret_cast<float *>(lds + a.k * pitch);
+    constexpr int U = 8;
+    u4 w[U];
+    float s[U];
+    // item: choice item / chunks, channels 1024 (item % chunks) + 16 lane; without a term: times 0
+    auto load = [&](int32_t first) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t item = min(first + u, items - 1), j = item / chunks, k = (item - j * chunks) * 1024 + lane * 16;
+            const int32_t e = ids[j], at = min(k, pitch - 16);
+            const bool there = first + u < items && k < pitch && e >= 0 && e < a.experts;
+            const int64_t of = e >= 0 && e < a.experts ? e : 0;
+            w[u] = stream16(a.w2 + (of * a.hidden + ch) * pitch + at);
+            s[u] = there ? a.s2[(of * a.hb + ch / kBlock) * a.ib + at / kBlock] * weights[j] : 0.0f;
+        }
+    };
+    load(0);
+    const int l = threadIdx.x & 15;
+    for (int32_t i = threadIdx.x >> 4; i < a.k * a.ib; i += 512 / 16) {
+        const int32_t j = i / a.ib, c = (i - j * a.ib) * kBlock + 8 * l;
+        float v[8];
+        // rows of ids that are no expert's were not written: zeros
+        const bool there = static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(a.experts);
+        load8_tail(a.h + (static_cast<int64_t>(token) * a.k + j) * a.inner + c, there ? a.inner - c : 0, a.inner % 4 == 0, v);
+        uint32_t m = most8(v);
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2)
+            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
+        const Scale q = scale_of(m);
+        *reinterpret_cast<u2 *>(lds + j * pitch + c) = u2{codes4(v, q.inv), codes4(v + 4, q.inv)};
+        if (l == 0)
+            scales[i] = q.scale;
+    }
+    __syncthreads();
+    float acc = 0.0f;
+    for (int32_t first = 0; first < items; first += U) {
+        if (first > 0)
+            load(first);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t item = min(first + u, items - 1), j = item / chunks;
+            const int32_t at = min((item - j * chunks) * 1024 + lane * 16, pitch - 16);
+            float v[16];
+            code_values(*reinterpret_cast<const u4 *>(lds + j * pitch + at), v);
+            const float d = dot16(v, w[u]) * (scales[j * a.ib + at / kBlock] * s[u]);
+            acc += s[u] != 0.0f ? d : 0.0f;
+        }
+    }
+    acc = sum_lanes(acc);
+    if (lane == 0 && static_cast<int32_t>(blockIdx.x) * 8 + wave < a.hidden)
+        store4(a.y, a.type, static_cast<int64_t>(token) * a.hidden + ch, f4{acc, 0, 0, 0}, 1, false);
 }
 
 // y[t] = sum_j weights[t][j] * z[place of (t, j)], in 32 bits, in the order of
@@ -486,60 +626,58 @@ hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
 }
 
 template <typename T>
-hipError_t gated_few(const ExpertArgs &a, bool direct, hipStream_t stream) {
-    const int32_t columns = (a.inner + 15) / 16;
+hipError_t gated_tokens(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
-    const int waves = std::min(a.hb, 8);
-    const size_t lds = static_cast<size_t>(waves) * 2048;
-    if (direct)
-        gated_stream<T, 2, true><<<dim3(columns, a.pairs), waves * 64, lds, stream>>>(a, columns, wide);
-    else
-        gated_stream<T, 2, false><<<tile_grid(most_tiles(a, 16), columns), waves * 64, lds, stream>>>(a, columns, wide);
+    const int32_t channels = 4 * kTokenChannels;
+    gated_token<T><<<dim3((a.inner + channels - 1) / channels, a.pairs), 256, 0, stream>>>(a, wide);
     return hipGetLastError();
-}
-
-hipError_t gated_few(const ExpertArgs &a, bool direct, hipStream_t stream) {
-    return a.type == kF32 ? gated_few<float>(a, direct, stream)
-           : a.type == kF16 ? gated_few<_Float16>(a, direct, stream)
-                            : gated_few<__bf16>(a, direct, stream);
 }
 
 }  // namespace
 
-ExpertPath expert_path(int32_t n, int32_t k, int32_t experts) {
+ExpertPath expert_path(int32_t n, int32_t k, int32_t experts, int32_t inner) {
     const int64_t pairs = static_cast<int64_t>(n) * k;
-    if (n <= 4 && pairs <= 64)
+    if (n <= 4 && pairs <= 64 && k * blocks_of(inner) <= 384)  // a token's inner rows in 50 KB of LDS
         return ExpertPath::kTokens;
     return pairs <= 16ll * experts ? ExpertPath::kFew : ExpertPath::kTiles;
 }
 
 hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
-    const ExpertPath path = expert_path(a.n, a.k, a.experts);
+    const ExpertPath path = expert_path(a.n, a.k, a.experts, a.inner);
     hipError_t e;
     if (path == ExpertPath::kTokens) {
-        if ((e = gated_few(a, true, stream)) != hipSuccess)
+        e = a.type == kF32   ? gated_tokens<float>(a, stream)
+            : a.type == kF16 ? gated_tokens<_Float16>(a, stream)
+                             : gated_tokens<__bf16>(a, stream);
+        if (e != hipSuccess)
             return e;
-        const int waves = std::min(a.k * a.ib, 16);
-        down_token<<<dim3((a.hidden + 15) / 16, a.n), waves * 64, waves * 1024, stream>>>(a, wide);
+        const int32_t blocks = a.k * a.ib;
+        down_token<<<dim3((a.hidden + 7) / 8, a.n), 512, blocks * (kBlock + 4), stream>>>(a);
         return hipGetLastError();
     }
-    if ((e = launch_sort_pairs(a.ids, a.pairs, a.experts, a.order, a.place, a.offsets, stream)) != hipSuccess)
+    if ((e = launch_sort_pairs(a.ids, a.pairs, a.experts, a.order, a.place, a.offsets, stream)) != hipSuccess ||
+        (e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
         return e;
     if (path == ExpertPath::kFew) {
-        if ((e = gated_few(a, false, stream)) != hipSuccess)
+        const int64_t tiles = most_tiles(a, 16);
+        const int32_t up = (a.inner + 15) / 16, down = (a.hidden + 15) / 16;
+        int waves = std::min(a.hb, 8);
+        if (a.hb > waves)
+            gated_rows<2><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
+        else
+            gated_rows<1><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
+        if ((e = hipGetLastError()) != hipSuccess ||
+            (e = launch_quantize_rows(a.h, kF32, a.inner, a.pairs, a.inner, a.hq, a.hs, stream)) != hipSuccess)
             return e;
-        const int32_t columns = (a.hidden + 31) / 32;
-        const int waves = std::min(a.ib, 8);
-        down_stream<2, 1><<<tile_grid(most_tiles(a, 16), columns), waves * 64, waves * 2048, stream>>>(a, columns);
+        waves = std::min((a.ib + 1) / 2, 8);
+        down_rows<2><<<tile_grid(tiles, down), waves * 64, waves * 1024, stream>>>(a, down);
         e = hipGetLastError();
     } else {
         using Small = TileShape<256, 64, 2, 4>;
         using Mid = TileShape<256, 128, 2, 4>;
         using Big = TileShape<256, 256, 2, 4>;
         const int64_t each = a.pairs / a.experts;
-        if ((e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
-            return e;
         // bf16: what the 8-bit instruction loses lies below the rounding of the result, f16 results
         // between the products and their sum as well
         if (a.type == kBf16)
