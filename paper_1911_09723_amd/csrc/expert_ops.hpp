@@ -59,11 +59,6 @@ constexpr int32_t kMostExperts = 1024;
 constexpr int32_t kMostChoices = 64;
 hipError_t launch_route(RouteArgs a, int32_t type, hipStream_t stream);
 
-// Pairs (token, choice) sorted by expert, stable: order[place] = pair, place[pair]
-// (-1: its id is no expert), offsets[experts + 1] = each expert's first place.
-hipError_t launch_sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order, int32_t *place,
-                             int32_t *offsets, hipStream_t stream);
-
 // The experts' networks over pairs (token, choice), pairs = n k.
 struct ExpertArgs {
     const void *x;             // [n][hidden], row stride ldx elements
@@ -76,7 +71,8 @@ struct ExpertArgs {
     int32_t type;              // of x and y
     int32_t n, k, pairs, experts, hidden, inner;
     int32_t hb, ib;            // blocks of 128 hidden and inner channels
-    // workspace: the pairs' order by expert, x's codes, the inner rows in 32 bits and
+    // workspace: the pairs sorted by expert (order[place] = pair, place[pair], -1 where
+    // the id is no expert, offsets[experts + 1] = each expert's first place), x's codes, the inner rows in 32 bits and
     // as codes, and the results, by place (token by token: by pair)
     int32_t *order, *place, *offsets;
     uint8_t *xq, *hq;

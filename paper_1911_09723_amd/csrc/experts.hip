@@ -14,6 +14,112 @@ namespace {
 
 constexpr int kXcds = 8;
 
+// Pairs (token, choice) sorted by expert: workgroup e finds the places of expert
+// e's pairs.  It counts, over all pairs, those of lower experts (its first place)
+// and its own, then hands out its places in the order of the pairs; no workgroup
+// waits for another, and no place depends on timing.  A wavefront walks its
+// share of the pairs 256 at a time, four neighbours a lane; the first kKept
+// pieces stay in registers for the second walk.
+__device__ __forceinline__ void sort_pairs(const ExpertArgs &a, int32_t e, bool wide) {
+    __shared__ int32_t part[2][16];
+    constexpr int kKept = 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int32_t pieces = (a.pairs + 255) / 256, per = (pieces + waves - 1) / waves;
+    const int32_t first = min(wave * per, pieces), last = min(first + per, pieces);
+    // four ids from pair 4 lane of a piece; past the end: none
+    auto load = [&](int32_t piece) {
+        const int32_t i = piece * 256 + lane * 4;
+        if (wide && i + 4 <= a.pairs)
+            return *reinterpret_cast<const i4 *>(a.ids + i);
+        i4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = i + j < a.pairs ? a.ids[i + j] : -1;
+        return v;
+    };
+    int32_t below = 0, own = 0;
+    auto count = [&](i4 v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            below += static_cast<uint32_t>(v[j]) < static_cast<uint32_t>(e);
+            own += v[j] == e;
+        }
+    };
+    i4 kept[kKept];
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+        kept[i] = first + i < last ? load(first + i) : i4{-1, -1, -1, -1};
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+        count(kept[i]);
+#pragma unroll 4
+    for (int32_t p = first + kKept; p < last; ++p)
+        count(load(p));
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        own += __shfl_xor(own, s);
+        below += __shfl_xor(below, s);
+    }
+    if (lane == 0) {
+        part[0][wave] = own;
+        part[1][wave] = below;
+    }
+    __syncthreads();
+    const int32_t owns = lane < waves ? part[0][lane] : 0;
+    int32_t start = lane < waves ? part[1][lane] : 0, total = start + owns;
+    start += lane < wave ? owns : 0;
+#pragma unroll
+    for (int s = 1; s < 16; s *= 2) {
+        start += __shfl_xor(start, s);
+        total += __shfl_xor(total, s);
+    }
+    int32_t at = __builtin_amdgcn_readfirstlane(start);
+    if (threadIdx.x == 0) {
+        a.offsets[e + 1] = total;
+        if (e == 0)
+            a.offsets[0] = 0;
+    }
+    auto give = [&](int32_t p, i4 v) {
+        const int32_t i = p * 256 + lane * 4;
+        int32_t before = at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint64_t mine = __ballot(v[j] == e);
+            before += __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mine >> 32),
+                                                __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mine), 0));
+            at += __popcll(mine);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (v[j] == e) {
+                a.order[before] = i + j;
+                a.place[i + j] = before++;
+            } else if (e == 0 && i + j < a.pairs && static_cast<uint32_t>(v[j]) >= static_cast<uint32_t>(a.experts)) {
+                a.place[i + j] = -1;
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+        if (first + i < last)
+            give(first + i, kept[i]);
+    for (int32_t p = first + kKept; p < last; ++p)
+        give(p, load(p));
+}
+
+// The sort and x's rows to codes, which do not need each other, in one launch:
+// workgroups below a.experts sort.
+template <typename T, int U>
+__global__ void __launch_bounds__(1024) prepare_rows(ExpertArgs a, int32_t row_groups, bool wide_ids, bool wide) {
+    if (static_cast<int32_t>(blockIdx.x) < a.experts) {
+        sort_pairs(a, blockIdx.x, wide_ids);
+        return;
+    }
+    const int32_t id = static_cast<int32_t>(blockIdx.x) - a.experts, part = id / row_groups;
+    quantize_group<T, U>(static_cast<const T *>(a.x), a.ldx, a.n, a.hidden, a.xq, a.xs, a.hb, id - part * row_groups, part,
+                         wide);
+}
+
 // g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each.
 // EXACT: g log2(e) is taken to twice 32 bits so that the exponential stays
 // there; else it is up to |g| last places off, far less than 8-bit products are.
@@ -626,6 +732,25 @@ hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
 }
 
 template <typename T>
+hipError_t prepare(const ExpertArgs &a, hipStream_t stream) {
+    const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
+    const bool wide_ids = reinterpret_cast<uintptr_t>(a.ids) % 16 == 0;
+    const int32_t threads = a.pairs >= 4096 ? 1024 : 256;
+    const int32_t groups = (a.n + threads / 16 - 1) / (threads / 16);
+    if (static_cast<int64_t>(groups) * a.hb >= 1024)
+        prepare_rows<T, 4><<<a.experts + groups * ((a.hb + 3) / 4), threads, 0, stream>>>(a, groups, wide_ids, wide);
+    else
+        prepare_rows<T, 1><<<a.experts + groups * a.hb, threads, 0, stream>>>(a, groups, wide_ids, wide);
+    return hipGetLastError();
+}
+
+// Wavefronts that share `blocks` evenly: at most 8, and two blocks each before that many.
+int even_waves(int32_t blocks) {
+    const int32_t each = std::max((blocks + 7) / 8, std::min(blocks, 2));
+    return (blocks + each - 1) / each;
+}
+
+template <typename T>
 hipError_t gated_tokens(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
     const int32_t channels = 4 * kTokenChannels;
@@ -656,21 +781,18 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         down_token<<<dim3((a.hidden + 7) / 8, a.n), 512, blocks * (kBlock + 4), stream>>>(a);
         return hipGetLastError();
     }
-    if ((e = launch_sort_pairs(a.ids, a.pairs, a.experts, a.order, a.place, a.offsets, stream)) != hipSuccess ||
-        (e = launch_quantize_rows(a.x, a.type, a.ldx, a.n, a.hidden, a.xq, a.xs, stream)) != hipSuccess)
+    e = a.type == kF32 ? prepare<float>(a, stream) : a.type == kF16 ? prepare<_Float16>(a, stream) : prepare<__bf16>(a, stream);
+    if (e != hipSuccess)
         return e;
     if (path == ExpertPath::kFew) {
         const int64_t tiles = most_tiles(a, 16);
         const int32_t up = (a.inner + 15) / 16, down = (a.hidden + 15) / 16;
-        int waves = std::min(a.hb, 8);
-        if (a.hb > waves)
-            gated_rows<2><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
-        else
-            gated_rows<1><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
+        int waves = even_waves(a.hb);
+        gated_rows<2><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
         if ((e = hipGetLastError()) != hipSuccess ||
             (e = launch_quantize_rows(a.h, kF32, a.inner, a.pairs, a.inner, a.hq, a.hs, stream)) != hipSuccess)
             return e;
-        waves = std::min((a.ib + 1) / 2, 8);
+        waves = even_waves(a.ib);
         down_rows<2><<<tile_grid(tiles, down), waves * 64, waves * 1024, stream>>>(a, down);
         e = hipGetLastError();
     } else {

@@ -110,6 +110,42 @@ __device__ __forceinline__ Scale scale_of(uint32_t most) {
     return {a / kTop, kTop / a};
 }
 
+// Rows to codes: 16 lanes hold a block of 128 (8 values each), a workgroup covers
+// blockDim / 16 rows, so that the scales of one channel block, which lie by row,
+// leave it as neighbouring bytes.  Each lane group walks U blocks of its row at
+// once to keep several loads in flight.  `group`: rows of this workgroup, in
+// workgroups; `part`: its blocks, in U.
+template <typename T, int U>
+__device__ __forceinline__ void quantize_group(const T *x, int64_t ldx, int32_t rows, int32_t cols, uint8_t *q,
+                                               float *scale, int32_t kb, int32_t group, int32_t part, bool wide) {
+    const int32_t row = group * static_cast<int32_t>(blockDim.x >> 4) + (threadIdx.x >> 4);
+    const int l = threadIdx.x & 15;
+    if (row >= rows)
+        return;
+    const T *xr = x + row * ldx;
+    const int32_t b0 = part * U;
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t c = (b0 + u) * kBlock + 8 * l;
+        load8_tail(xr + c, cols - c, wide, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (b0 + u >= kb)
+            break;
+        uint32_t m = most8(v[u]);
+#pragma unroll
+        for (int s = 1; s < 16; s *= 2)
+            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), s)));
+        const Scale s = scale_of(m);
+        const int64_t at = (static_cast<int64_t>(row) * kb + b0 + u) * kBlock + 8 * l;
+        *reinterpret_cast<u2 *>(q + at) = u2{codes4(v[u], s.inv), codes4(v[u] + 4, s.inv)};
+        if (l == 0)
+            scale[static_cast<int64_t>(b0 + u) * rows + row] = s.scale;
+    }
+}
+
 // Products.  p (16 x 16, f4 a lane) = A (16 rows x 128) B (16 columns x 128):
 // lane l holds of each operand row l % 16, bytes 16 (l / 16) .. + 15 and 64
 // further on (any places, the same for both), and of the result column (B)

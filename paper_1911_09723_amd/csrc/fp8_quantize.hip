@@ -10,40 +10,12 @@
 namespace spconv {
 namespace {
 
-// Rows.  16 lanes hold a block of 128 (8 values each); a workgroup covers 16
-// rows, so that the scales of one channel block, which lie by row, leave it as
-// 64 neighbouring bytes.  Each lane group walks U blocks of its row at a time
-// to keep several loads in flight.
 template <typename T, int U>
 __global__ void __launch_bounds__(256) quantize_rows(const T *x, int64_t ldx, int32_t rows, int32_t cols, uint8_t *q,
                                                      float *scale, int32_t kb, int32_t row_groups, bool wide) {
     const int32_t part = static_cast<int32_t>(blockIdx.x) / row_groups;
-    const int32_t row = (static_cast<int32_t>(blockIdx.x) - part * row_groups) * 16 + (threadIdx.x >> 4);
-    const int l = threadIdx.x & 15;
-    if (row >= rows)
-        return;
-    const T *xr = x + row * ldx;
-    const int32_t b0 = part * U;
-    float v[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int32_t c = (b0 + u) * kBlock + 8 * l;
-        load8_tail(xr + c, cols - c, wide, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (b0 + u >= kb)
-            break;
-        uint32_t m = most8(v[u]);
-#pragma unroll
-        for (int s = 1; s < 16; s *= 2)
-            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), s)));
-        const Scale s = scale_of(m);
-        const int64_t at = (static_cast<int64_t>(row) * kb + b0 + u) * kBlock + 8 * l;
-        *reinterpret_cast<u2 *>(q + at) = u2{codes4(v[u], s.inv), codes4(v[u] + 4, s.inv)};
-        if (l == 0)
-            scale[static_cast<int64_t>(b0 + u) * rows + row] = s.scale;
-    }
+    quantize_group<T, U>(x, ldx, rows, cols, q, scale, kb, static_cast<int32_t>(blockIdx.x) - part * row_groups, part,
+                         wide);
 }
 
 // Blocks of 128 x 128, one a workgroup: a thread holds 8 values of 8 rows.

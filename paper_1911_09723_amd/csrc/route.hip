@@ -1,4 +1,4 @@
-// The experts of each token, and the order of the rows that they work on.
+// The experts of each token.
 //
 // Routing: s = softmax(l) or 1 / (1 + exp(-l)) over a token's logits, value =
 // s + bias; experts in equal groups, a group's rank is the sum of its one or
@@ -192,84 +192,6 @@ __global__ void __launch_bounds__(256) route_kernel(RouteArgs a, bool wide) {
     }
 }
 
-// Rows by expert: workgroup e finds the places of expert e's pairs (token,
-// choice) in the order of all pairs sorted by expert.  It counts, over all
-// pairs, those of lower experts (its first place) and its own, then hands out
-// its places in the order of the pairs; no workgroup waits for another, and no
-// place depends on timing.  A wavefront walks its share of the pairs 256 at a
-// time, four neighbours a lane, twice.
-__global__ void __launch_bounds__(1024) sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order,
-                                                   int32_t *place, int32_t *offsets, bool wide) {
-    __shared__ int32_t part[2][16];
-    const int32_t e = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int32_t pieces = (pairs + 255) / 256, per = (pieces + waves - 1) / waves;
-    const int32_t first = min(wave * per, pieces), last = min(first + per, pieces);
-    // four ids from pair 4 lane of a piece; past the end: none
-    auto load = [&](int32_t piece) {
-        const int32_t i = piece * 256 + lane * 4;
-        if (wide && i + 4 <= pairs)
-            return *reinterpret_cast<const i4 *>(ids + i);
-        i4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = i + j < pairs ? ids[i + j] : -1;
-        return v;
-    };
-    int32_t below = 0, own = 0;
-#pragma unroll 4
-    for (int32_t p = first; p < last; ++p) {
-        const i4 v = load(p);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            below += static_cast<uint32_t>(v[j]) < static_cast<uint32_t>(e);
-            own += v[j] == e;
-        }
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-        own += __shfl_xor(own, s);
-        below += __shfl_xor(below, s);
-    }
-    if (lane == 0) {
-        part[0][wave] = own;
-        part[1][wave] = below;
-    }
-    __syncthreads();
-    int32_t at = 0, total = 0;
-    for (int w = 0; w < waves; ++w) {
-        at += part[1][w] + (w < wave ? part[0][w] : 0);
-        total += part[1][w] + part[0][w];
-    }
-    if (threadIdx.x == 0) {
-        offsets[e + 1] = total;
-        if (e == 0)
-            offsets[0] = 0;
-    }
-#pragma unroll 4
-    for (int32_t p = first; p < last; ++p) {
-        const i4 v = load(p);
-        const int32_t i = p * 256 + lane * 4;
-        int32_t before = at;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint64_t mine = __ballot(v[j] == e);
-            before += __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mine >> 32),
-                                                __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mine), 0));
-            at += __popcll(mine);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (v[j] == e) {
-                order[before] = i + j;
-                place[i + j] = before++;
-            } else if (e == 0 && i + j < pairs && static_cast<uint32_t>(v[j]) >= static_cast<uint32_t>(experts)) {
-                place[i + j] = -1;
-            }
-        }
-    }
-}
-
 template <typename T, int PER>
 hipError_t route_per(const RouteArgs &a, hipStream_t stream) {
     const int64_t piece = static_cast<int64_t>(sizeof(T)) * PER;
@@ -300,14 +222,6 @@ hipError_t launch_route(RouteArgs a, int32_t type, hipStream_t stream) {
     return type == kF32 ? route_of<float>(a, stream)
            : type == kF16 ? route_of<_Float16>(a, stream)
                           : route_of<__bf16>(a, stream);
-}
-
-hipError_t launch_sort_pairs(const int32_t *ids, int32_t pairs, int32_t experts, int32_t *order, int32_t *place,
-                             int32_t *offsets, hipStream_t stream) {
-    const int32_t threads = pairs >= 4096 ? 1024 : pairs > 256 ? 256 : 64;
-    sort_pairs<<<experts, threads, 0, stream>>>(ids, pairs, experts, order, place, offsets,
-                                                reinterpret_cast<uintptr_t>(ids) % 16 == 0);
-    return hipGetLastError();
 }
 
 }  // namespace spconv
