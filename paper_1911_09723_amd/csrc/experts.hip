@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
                 a.zs[static_cast<int64_t>(tile.row + r) * a.hb + cw / kBlock] = p.value;
         }
     }
-    store_tile<S>(acc, a.z, HALF ? kF16 : kF32, tile.row, tile.rows, ch, a.hidden, a.hidden % 4 == 0, wt, lane,
+    store_tile<S>(acc, a.z, HALF ? kF16 : kF32, tile.row, tile.rows, ch, a.hidden, a.hidden % 4 == 0, wave, lane, lds,
                   [&](f4 v, int, int t) { return HALF ? v * inverse[t] : v; });
 }
 

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     from.xs_at = min(t0 + wave * 64 + lane, a.n - 1) * 4u;
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.kb;
-    const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
+    const int wc = channel_part<S>(wave);
     const int32_t cw = c0 + wc * S::NC * 16;
     const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
     f4 acc[S::NC][S::NT] = {};
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     for (int c = 0; c < S::NC; ++c)
         bias[c] = bias4(a.bias, ch + c * 16, a.cout);
     const bool clamp = a.lo > -INFINITY || a.hi < INFINITY;
-    store_tile<S>(acc, a.y, a.y_type, t0, a.n - t0, ch, a.cout, wide, wt, lane, [&](f4 v, int c, int) {
+    store_tile<S>(acc, a.y, a.y_type, t0, a.n - t0, ch, a.cout, wide, wave, lane, lds, [&](f4 v, int c, int) {
         v += bias[c];
         if (clamp)
 #pragma unroll
