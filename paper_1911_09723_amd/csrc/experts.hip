@@ -147,24 +147,28 @@ struct RowTile {
     int32_t expert, row, rows;
 };
 
-// Tile `id` of all (tile of `high` rows, column tile of `wide`), in the order
-// that gives each XCD one run of neighbouring tiles: tiles of one expert share
-// its weights, and column tiles the rows, in an L2.  False past the last one.
-// Every lane takes 64th expert; the scans are over a wavefront.
+// This workgroup's tile of all (tiles of `high` rows, `wide` column tiles each),
+// in the order that gives each XCD one run of neighbouring tiles: tiles of one
+// expert share its weights, and column tiles the rows, in an L2.  False past the
+// last one.  Lanes take experts 64 at a time; what leaves is the same in all of
+// them and is kept in scalar registers (readfirstlane, readlane), where the
+// tile's buffer resources have to be: a resource that the compiler takes to
+// differ between lanes costs a loop around every load.
 __device__ __forceinline__ bool find_tile(const int32_t *offsets, int32_t experts, int32_t high, int32_t wide,
                                           int lane, RowTile *tile, int32_t *column) {
     auto tiles_of = [&](int32_t e) {
         return e < experts ? (offsets[e + 1] - offsets[e] + high - 1) / high : 0;
     };
-    int32_t total = 0;
+    int32_t sum = 0;
     for (int32_t e0 = 0; e0 < experts; e0 += 64)
-        total += tiles_of(e0 + lane);
+        sum += tiles_of(e0 + lane);
 #pragma unroll
     for (int s = 1; s < 64; s *= 2)
-        total += __shfl_xor(total, s);
-    const int32_t per = (total * wide + kXcds - 1) / kXcds;
+        sum += __shfl_xor(sum, s);
+    const int32_t total = __builtin_amdgcn_readfirstlane(sum) * wide;
+    const int32_t per = (total + kXcds - 1) / kXcds;
     const int32_t in = blockIdx.x / kXcds, id = blockIdx.x % kXcds * per + in;
-    if (in >= per || id >= total * wide)
+    if (in >= per || id >= total)
         return false;
     int32_t want = id / wide;
     *column = id - want * wide;
@@ -179,15 +183,13 @@ __device__ __forceinline__ bool find_tile(const int32_t *offsets, int32_t expert
         const uint64_t past = __ballot(upto > want);
         if (past) {
             const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            const int32_t before = __shfl(upto - own, at);
-            tile->expert = __builtin_amdgcn_readfirstlane(e0 + at);
-            const int32_t row = offsets[tile->expert] + (want - before) * high;
-            tile->row = __builtin_amdgcn_readfirstlane(row);
-            tile->rows = __builtin_amdgcn_readfirstlane(min(high, offsets[tile->expert + 1] - row));
-            *column = __builtin_amdgcn_readfirstlane(*column);
+            const int32_t before = __builtin_amdgcn_readlane(upto - own, at);
+            tile->expert = e0 + at;
+            tile->row = uniform_load(offsets + tile->expert) + (want - before) * high;
+            tile->rows = min(high, uniform_load(offsets + tile->expert + 1) - tile->row);
             return true;
         }
-        want -= __shfl(upto, 63);
+        want -= __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     }
     from.rows = tile.rows;
     from.xs = a.xs;
-    from.xs_at = wave < S::BT / 64 ? a.order[tile.row + min(wave * 64 + lane, tile.rows - 1)] / a.k * 4u : 0;
+    from.xs_at = a.order[tile.row + min(wave % (S::BT / 64) * 64 + lane, tile.rows - 1)] / a.k * 4u;
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
@@ -315,7 +317,7 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
     }
     from.rows = tile.rows;
     from.xs = a.hs + tile.row;
-    from.xs_at = min(wave * 64 + lane, tile.rows - 1) * 4u;
+    from.xs_at = min(wave % (S::BT / 64) * 64 + lane, tile.rows - 1) * 4u;
     from.xs_step = a.pairs * 4u;
     from.xs_bytes = from.xs_step * (a.ib - 1) + tile.rows * 4u;
     const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
@@ -800,20 +802,25 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         using Mid = TileShape<256, 128, 2, 4>;
         using Big = TileShape<256, 256, 2, 4>;
         const int64_t each = a.pairs / a.experts;
-        // bf16: what the 8-bit instruction loses lies below the rounding of the result, f16 results
-        // between the products and their sum as well
+        // The inner rows are rounded to codes again, which turns an error of 4e-5 into one of
+        // 1.5e-3: below the rounding of bf16 results, not of others, whose first products are exact.
+        // The results' error is their own: exact products for 32 bits only.
         if (a.type == kBf16)
             e = each >= 192  ? gated_tiles<Big, false>(a, stream)
                 : each >= 96 ? gated_tiles<Mid, false>(a, stream)
                              : gated_tiles<Small, false>(a, stream);
         else
-            e = gated_tiles<Small, true>(a, stream);
+            e = each >= 96 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
         if (e != hipSuccess)
             return e;
         if (a.type == kF32)
-            e = down_tiles<TileShape<128, 128, 2, 2>, true, false>(a, stream);
+            e = each >= 192  ? down_tiles<Big, true, false>(a, stream)
+                : each >= 96 ? down_tiles<Mid, true, false>(a, stream)
+                             : down_tiles<Small, true, false>(a, stream);
         else if (a.type == kF16)
-            e = each >= 96 ? down_tiles<Mid, false, false>(a, stream) : down_tiles<Small, false, false>(a, stream);
+            e = each >= 192  ? down_tiles<Big, false, false>(a, stream)
+                : each >= 96 ? down_tiles<Mid, false, false>(a, stream)
+                             : down_tiles<Small, false, false>(a, stream);
         else
             e = each >= 192  ? down_tiles<Big, false, true>(a, stream)
                 : each >= 96 ? down_tiles<Mid, false, true>(a, stream)

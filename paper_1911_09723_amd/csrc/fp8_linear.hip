@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     }
     from.rows = a.n - t0;
     from.xs = a.xs;
-    from.xs_at = min(t0 + wave * 64 + lane, a.n - 1) * 4u;
+    from.xs_at = min(t0 + wave % (S::BT / 64) * 64 + lane, a.n - 1) * 4u;
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.kb;
     const int wc = channel_part<S>(wave);
@@ -149,14 +149,14 @@ __global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x,
     });
 }
 
-constexpr int32_t kStreamRows = 64;     // most rows that take the stream kernel
+constexpr int32_t kStreamRows = 32;     // most rows that take the stream kernel
 constexpr int32_t kStreamQuantize = 16; // most rows that it quantises itself
 
 size_t size_of(int32_t type) { return type == kF32 ? 4 : type == kFp8 ? 1 : 2; }
 
 template <typename XT, int TT>
 hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_t stream) {
-    const int waves = std::min(a.kb, TT == 4 ? 8 : 16);
+    const int waves = std::min(a.kb, 16);
     const dim3 grid((a.cout + 15) / 16, (a.n + 16 * TT - 1) / (16 * TT));
     const size_t lds = static_cast<size_t>(waves) * TT * 1024;
     if (a.kb > waves)
@@ -183,6 +183,15 @@ hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream) {
 
 bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) { return n <= kStreamQuantize; }
 
+// Which kernel.  Up to 32 rows the stream kernel: the weight's bytes bound it (24 x 4096 ->
+// 4096: 8.7 us, the smallest tiles 11.5; 64 rows 14.5 and 11.5).  Then tiles, the largest that
+// still give the card's 256 compute units work: a tile of 64 x 64 four blocks deep where there
+// are no more of those than compute units (128 rows of 4096 -> 4096: 11.7 us against 15.2 in
+// tiles of 128 x 64), 256 x 256 from 112 on (2048 rows: 47.8 against 52.1; 1536: 39.4 against 39.0
+// with 96), 128 x 64 between, three blocks deep while a compute unit has one (512 rows: 17.0
+// against 22.3 two deep; 1024 rows, two each: 27.7 against 25.9).  Results in 32 bits take the
+// exact products, at half the rate: 256 x 256 from 192 on (2048 rows, 128 tiles: 97 us against 69
+// in tiles of 128 x 128; 8192 rows, 512 tiles: 207 against 252).
 hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
     const bool wide_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size_of(a.x_type) % 16 == 0;
     const bool wide = a.cout % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
@@ -192,15 +201,23 @@ hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
                                   : stream_launch<__bf16, 1>(a, wide_x, wide, stream);
     if (a.n <= 16)
         return stream_launch<Fp8, 1>(a, wide_x, wide, stream);
-    if (a.n <= 32)
-        return stream_launch<Fp8, 2>(a, wide_x, wide, stream);
     if (a.n <= kStreamRows)
-        return stream_launch<Fp8, 4>(a, wide_x, wide, stream);
-    if (a.y_type == kF32)
-        return tile_launch<TileShape<128, 128, 2, 2>, true>(a, wide, stream);
-    if (static_cast<int64_t>((a.cout + 255) / 256) * ((a.n + 255) / 256) >= 192)
-        return tile_launch<TileShape<256, 256, 2, 4>, false>(a, wide, stream);
-    return tile_launch<TileShape<128, 128, 2, 2>, false>(a, wide, stream);
+        return stream_launch<Fp8, 2>(a, wide_x, wide, stream);
+    auto tiles = [&](int32_t channels, int32_t rows) {
+        return static_cast<int64_t>((a.cout + channels - 1) / channels) * ((a.n + rows - 1) / rows);
+    };
+    const bool exact = a.y_type == kF32;
+    if (tiles(64, 64) <= 256)
+        return exact ? tile_launch<TileShape<64, 64, 1, 4, 4>, true>(a, wide, stream)
+                     : tile_launch<TileShape<64, 64, 1, 4, 4>, false>(a, wide, stream);
+    if (tiles(256, 256) >= (exact ? 192 : 112))
+        return exact ? tile_launch<TileShape<256, 256, 2, 4>, true>(a, wide, stream)
+                     : tile_launch<TileShape<256, 256, 2, 4>, false>(a, wide, stream);
+    if (tiles(128, 64) <= 256)
+        return exact ? tile_launch<TileShape<128, 64, 2, 2, 3>, true>(a, wide, stream)
+                     : tile_launch<TileShape<128, 64, 2, 2, 3>, false>(a, wide, stream);
+    return exact ? tile_launch<TileShape<128, 128, 2, 2>, true>(a, wide, stream)
+                 : tile_launch<TileShape<128, 64, 2, 2>, false>(a, wide, stream);
 }
 
 }  // namespace spconv

@@ -19,7 +19,9 @@ namespace spconv {
 // Tile core.  BC channels x BT rows, WC x WT wavefronts, each NC x NT pieces of
 // 16 x 16.  Per block of 128 channels, BC + BT lines of 128 bytes and BT scales
 // go straight from global memory to LDS (16 bytes a lane, no registers between),
-// into the other of two buffers while the products of this one run.
+// STAGES - 1 blocks ahead of the products, into the buffer that the block before
+// has left; a block begins with one barrier, after each wavefront has seen its
+// own loads of that block arrive.
 //
 // A line's 16-byte pieces are stored in the order piece ^ (line / 2 % 8): 16
 // lanes that read one piece of 16 neighbouring lines then touch each of LDS's
@@ -40,7 +42,7 @@ namespace spconv {
 // 10 us of that, and half of what is left over the products' own 70 us is the
 // start of each block, where all wavefronts read their first operands at once.
 // ---------------------------------------------------------------------------
-template <int BC_, int BT_, int WC_, int WT_>
+template <int BC_, int BT_, int WC_, int WT_, int STAGES_ = 2>
 struct TileShape {
     static constexpr int BC = BC_, BT = BT_, WC = WC_, WT = WT_;
     static constexpr int kWaves = WC * WT, kThreads = 64 * kWaves;
@@ -49,8 +51,9 @@ struct TileShape {
     static constexpr int kLoads = kLines / 8 / kWaves;       // 8 lines an instruction
     static constexpr int kWeightLoads = BC / 8 / kWaves;     // the first of them: W's
     static constexpr int kStep = NC * NT >= 2 * kLoads ? 2 : 1;  // products from load to load
+    static constexpr int kStages = STAGES_;
     static constexpr int kStage = kLines * kBlock + BT * 4;
-    static constexpr int kLds = 2 * kStage;
+    static constexpr int kLds = kStages * kStage;
     static_assert(BC % (8 * kWaves) == 0 && BT % (8 * kWaves) == 0 && BT % 64 == 0 && BT / 64 <= kWaves &&
                       NC * NT >= kLoads, "whole loads a wavefront");
 };
@@ -90,8 +93,18 @@ __device__ __forceinline__ int channel_part(int wave) { return wave % S::WC; }
 template <class S>
 __device__ __forceinline__ int row_part(int wave) { return wave / S::WC; }
 
-__device__ __forceinline__ float uniform_load(const float *p) {
-    return *reinterpret_cast<const __attribute__((address_space(4))) float *>(reinterpret_cast<uintptr_t>(p));
+// A scalar load: of an address that is the same in all lanes, of what no kernel
+// in flight writes.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T *p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) T *>(reinterpret_cast<uintptr_t>(p));
+}
+
+// Waits until all but the last N of this wavefront's loads have arrived and all
+// its reads of LDS are done, then for the workgroup's other wavefronts.
+template <int N>
+__device__ __forceinline__ void wait_all() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // acc[c][t] += the products over kb blocks; ws0, ws1: the scales by block of
@@ -103,24 +116,43 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
                                              unsigned char *lds, int wave, int lane) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources
     const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
-    auto load = [&](int i, Rsrc w, Rsrc x, int32_t b, unsigned char *buf) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            i < S::kWeightLoads ? w : x,
-            (__attribute__((address_space(3))) void *)(buf + (wave + i * S::kWaves) * 1024), 16, from.at[i], b * kBlock, 0,
-            0);
-    };
-    auto load_scales = [&](Rsrc xs, int32_t b, unsigned char *buf) {
-        if (wave < S::BT / 64)
+    // Every wavefront issues the same number of loads a block, so that it can
+    // count them: kLoads of lines, one of scales (the first BT / 64 wavefronts',
+    // by the others again).  Past the last block they are out of their range and
+    // read nothing.
+    constexpr int kEach = S::kLoads + 1;
+    auto load = [&](int i, int32_t b, unsigned char *buf) {
+        if (i < S::kLoads) {
+            const bool of_w = i < S::kWeightLoads;
+            const uint32_t bytes = of_w ? from.w_bytes : from.x_bytes;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                xs, (__attribute__((address_space(3))) void *)(buf + S::kLines * kBlock + wave * 256), 4, from.xs_at,
-                b * from.xs_step, 0, 0);
+                make_rsrc(of_w ? from.w : from.x, b < kb ? bytes : 0),
+                (__attribute__((address_space(3))) void *)(buf + (wave + i * S::kWaves) * 1024), 16, from.at[i],
+                b * kBlock, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                make_rsrc(from.xs, b < kb ? from.xs_bytes : 0),
+                (__attribute__((address_space(3))) void *)(buf + S::kLines * kBlock + wave % (S::BT / 64) * 256), 4,
+                from.xs_at, b * from.xs_step, 0, 0);
+        }
     };
-    {
-        const Rsrc w = make_rsrc(from.w, from.w_bytes), x = make_rsrc(from.x, from.x_bytes);
 #pragma unroll
-        for (int i = 0; i < S::kLoads; ++i)
-            load(i, w, x, 0, lds);
-        load_scales(make_rsrc(from.xs, from.xs_bytes), 0, lds);
+    for (int st = 0; st < S::kStages - 1; ++st)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            load(i, st, lds + st * S::kStage);
+    int32_t at_stage = 0, to_stage = (S::kStages - 1) * S::kStage;
+    auto next_stage = [](int32_t at) { return at == (S::kStages - 1) * S::kStage ? 0 : at + S::kStage; };
+    if (wt * S::NT * 16 >= from.rows) {  // no rows of its own: only its share of the loads
+        for (int32_t b = 0; b < kb; ++b) {
+            wait_all<(S::kStages - 2) * kEach>();
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                load(i, b + S::kStages - 1, lds + to_stage);
+            to_stage = next_stage(to_stage);
+        }
+        __syncthreads();
+        return;
     }
     // this lane's place in a piece of 16 lines: line lane % 16, 16-byte piece lane / 16 (and 4 further)
     const int at = (lane & 15) * kBlock + (((lane >> 4) ^ ((lane & 15) >> 1)) * 16);
@@ -128,26 +160,12 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
         return join(*reinterpret_cast<const u4 *>(p + at), *reinterpret_cast<const u4 *>(p + (at ^ 64)));
     };
     float sw0 = uniform_load(ws0), sw1 = HALVES ? uniform_load(ws1) : 0.0f;
-    __syncthreads();
-    if (wt * S::NT * 16 >= from.rows) {  // no rows of its own: only its share of the loads
-        for (int32_t b = 1; b < kb; ++b) {
-            const Rsrc w = make_rsrc(from.w, from.w_bytes), x = make_rsrc(from.x, from.x_bytes);
-#pragma unroll
-            for (int i = 0; i < S::kLoads; ++i)
-                load(i, w, x, b, lds + (b & 1) * S::kStage);
-            load_scales(make_rsrc(from.xs, from.xs_bytes), b, lds + (b & 1) * S::kStage);
-            __syncthreads();
-        }
-        __syncthreads();
-        return;
-    }
     for (int32_t b = 0; b < kb; ++b) {
-        const unsigned char *buf = lds + (b & 1) * S::kStage;
-        unsigned char *other = lds + (b + 1 & 1) * S::kStage;
-        // past the last block the loads are out of their range and read nothing
-        const bool more = b + 1 < kb;
-        const Rsrc w = make_rsrc(from.w, more ? from.w_bytes : 0), x = make_rsrc(from.x, more ? from.x_bytes : 0);
-        const Rsrc xs = make_rsrc(from.xs, more ? from.xs_bytes : 0);
+        wait_all<(S::kStages - 2) * kEach>();
+        const unsigned char *buf = lds + at_stage;
+        unsigned char *other = lds + to_stage;
+        at_stage = next_stage(at_stage);
+        to_stage = next_stage(to_stage);
         const unsigned char *wl = buf + wc * S::NC * 16 * kBlock;
         const unsigned char *xl = buf + (S::BC + wt * S::NT * 16) * kBlock;
         const float *sl = reinterpret_cast<const float *>(buf + S::kLines * kBlock) + wt * S::NT * 16 + (lane & 15);
@@ -183,12 +201,11 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
                     total[t] += s0[t];
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                constexpr int kStep = S::kStep;
                 const int id = c * S::NT + t;
-                if (id % kStep == kStep - 1 && id / kStep < S::kLoads)
-                    load(id / kStep, w, x, b + 1, other);
-                if (id == kStep * S::kLoads - 1)
-                    load_scales(xs, b + 1, other);
+#pragma unroll
+                for (int i = 0; i < kEach; ++i)
+                    if (id == min(i * S::kStep + S::kStep - 1, S::NC * S::NT - 1))
+                        load(i, b + S::kStages - 1, other);
                 __builtin_amdgcn_sched_barrier(0);
                 if (c > 0)
                     add(c - 1, t);
@@ -201,8 +218,8 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
         // the next block's scales: asked for here, so that no later wait for operands in LDS is one for them
         sw0 = uniform_load(ws0 + min(b + 1, kb - 1));
         sw1 = HALVES ? uniform_load(ws1 + min(b + 1, kb - 1)) : 0.0f;
-        __syncthreads();
     }
+    __syncthreads();
 #endif
 }
 

@@ -101,13 +101,16 @@ def test_linear_matches_64_bits(dtype, n, cin, cout, act, bias, extra):
     _check_linear(layer.run(x), x, layer, b, act, dtype)
 
 
-@pytest.mark.parametrize("n,cin,cout", [(4099, 384, 3073), (4096, 128, 4097), (12, 128, 70000), (70000, 128, 12)])
-def test_linear_many_rows_or_channels(n, cin, cout):
-    note("linear n %d cin %d cout %d" % (n, cin, cout))
+# every tile shape, and grids of several thousand tiles
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,cin,cout", [(70, 1300, 70), (300, 640, 2100), (1030, 384, 1030), (2050, 256, 2050),
+                                        (4099, 384, 3075), (12, 128, 70000), (70000, 128, 12)])
+def test_linear_many_rows_or_channels(dtype, n, cin, cout):
+    note("linear %s n %d cin %d cout %d" % (dtype, n, cin, cout))
     w, b = _layer(cout, cin, 3, True)
     layer = sp.Fp8Linear.from_dense(w, b)
-    x = _rows(n, cin, "bf16", 4)
-    _check_linear(layer.run(x), x, layer, b, "none", "bf16")
+    x = _rows(n, cin, dtype, 4)
+    _check_linear(layer.run(x), x, layer, b, "none", dtype)
 
 
 @pytest.mark.parametrize("n", [1, 16, 17, 40, 64, 65, 300])
