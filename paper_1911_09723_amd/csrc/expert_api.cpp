@@ -114,23 +114,19 @@ int64_t experts_layout(spconv::ExpertArgs &a, uint8_t *base) {
         at += (bytes + 255) / 256 * 256;  // codes on whole 128-byte lines: else a product reads two for one
     };
     const int64_t pairs = a.pairs;
-    const spconv::ExpertPath path = spconv::expert_path(a.n, a.k, a.experts, a.inner);
-    if (path != spconv::ExpertPath::kTokens) {
-        take(a.order, pairs * 4);
-        take(a.place, pairs * 4);
-        take(a.offsets, (a.experts + 1) * int64_t(4));
-        take(a.z, pairs * a.hidden * 4);
-        take(a.xq, code_bytes(a.n, a.hidden));
-        take(a.xs, static_cast<int64_t>(a.n) * a.hb * 4);
-    }
-    if (path == spconv::ExpertPath::kTiles)
-        take(a.zs, pairs * a.hb * 4);
-    if (path != spconv::ExpertPath::kTiles)
+    if (spconv::experts_by_token(a.n, a.k, a.experts, a.inner)) {
         take(a.h, pairs * a.inner * 4);
-    if (path != spconv::ExpertPath::kTokens) {
-        take(a.hq, code_bytes(pairs, a.inner));
-        take(a.hs, pairs * a.ib * 4);
+        return at;
     }
+    take(a.order, pairs * 4);
+    take(a.place, pairs * 4);
+    take(a.offsets, (a.experts + 1) * int64_t(4));
+    take(a.xq, code_bytes(a.n, a.hidden));
+    take(a.xs, static_cast<int64_t>(a.n) * a.hb * 4);
+    take(a.hq, code_bytes(pairs, a.inner));
+    take(a.hs, pairs * a.ib * 4);
+    take(a.z, pairs * a.hidden * 4);
+    take(a.zs, pairs * a.hb * 4);
     return at;
 }
 

@@ -72,8 +72,9 @@ struct ExpertArgs {
     int32_t n, k, pairs, experts, hidden, inner;
     int32_t hb, ib;            // blocks of 128 hidden and inner channels
     // workspace: the pairs sorted by expert (order[place] = pair, place[pair], -1 where
-    // the id is no expert, offsets[experts + 1] = each expert's first place), x's codes, the inner rows in 32 bits and
-    // as codes, and the results, by place (token by token: by pair)
+    // the id is no expert, offsets[experts + 1] = each expert's first place), x's codes,
+    // the inner rows' codes and the results by place; token by token only the inner rows,
+    // in 32 bits by pair (h)
     int32_t *order, *place, *offsets;
     uint8_t *xq, *hq;
     float *xs, *hs, *h;
@@ -81,10 +82,9 @@ struct ExpertArgs {
     float *zs;
 };
 
-// How a call is run: token by token (each pair reads its expert's weights), by
-// expert with the rows of 16 at a time against streamed weights, or over LDS tiles.
-enum class ExpertPath { kTokens, kFew, kTiles };
-ExpertPath expert_path(int32_t n, int32_t k, int32_t experts, int32_t inner);
+// Whether a call runs token by token, each pair reading its expert's weights, instead of
+// over tiles of the rows of one expert.
+bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner);
 hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream);
 
 }  // namespace spconv

@@ -343,133 +343,14 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
                   [&](f4 v, int, int t) { return HALF ? v * inverse[t] : v; });
 }
 
-// Few rows.  What bounds them is the weights' bytes, and a compute unit takes in
-// no more than its share of the card's rate (some 20 GB/s: what it can have
-// outstanding, over the memory's latency), so the weights have to be spread
-// evenly over all of them: workgroups of 16 channels (8 for single tokens), the
-// blocks of input channels dealt to their wavefronts.  Workgroups of 128
-// channels, which could convert the inner rows to codes themselves, took 24
-// instead of 14 us for the first products of one token (6 x 4 MB).
-
-// First products of up to 16 rows of one expert, given as codes: 16 gate and 16
-// up channels; the gated result leaves in 32 bits.
-template <int U>
-__global__ void __launch_bounds__(512) gated_rows(ExpertArgs a, int32_t columns) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int waves = blockDim.x >> 6;
-    RowTile tile;
-    int32_t column;
-    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &column))
-        return;
-    const int32_t c0 = column * 16;
-    const int64_t pitch = static_cast<int64_t>(a.hb) * kBlock;
-    const uint8_t *wg = a.w13 + (static_cast<int64_t>(tile.expert) * 2 * a.inner + min(c0 + (lane & 15), a.inner - 1)) * pitch;
-    const uint8_t *wu = wg + a.inner * pitch;
-    const float *sg = a.s13 + (static_cast<int64_t>(tile.expert) * 2 * a.ib + c0 / kBlock) * a.hb;
-    const float *su = sg + static_cast<int64_t>(a.ib) * a.hb;
-    const int32_t token = a.order[tile.row + min(lane & 15, tile.rows - 1)] / a.k;
-    const uint8_t *x = a.xq + token * pitch;
-    const float *xs = a.xs + token;
-    f4 acc[2] = {};
-    for (int32_t b0 = wave; b0 < a.hb; b0 += waves * U) {
-        i8 g[U], up[U];
-        RowPart xp[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = min(b0 + u * waves, a.hb - 1);
-            g[u] = weight_part(wg, b, lane);
-            up[u] = weight_part(wu, b, lane);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = min(b0 + u * waves, a.hb - 1);
-            xp[u] = row_codes(x, xs + static_cast<int64_t>(b) * a.n, b, lane);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = b0 + u * waves;
-            if (b >= a.hb)
-                break;
-            const Halves xh = halves(xp[u].code);
-            const f4 p = mfma128(halves(g[u]), xh), q = mfma128(halves(up[u]), xh);
-            const float s0 = xp[u].scale * uniform_load(sg + b), s1 = xp[u].scale * uniform_load(su + b);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[0][i] = fmaf(s0, p[i], acc[0][i]);
-                acc[1][i] = fmaf(s1, q[i], acc[1][i]);
-            }
-        }
-    }
-    f4 *all = reinterpret_cast<f4 *>(lds);
-    all[(wave * 2) * 64 + lane] = acc[0];
-    all[(wave * 2 + 1) * 64 + lane] = acc[1];
-    __syncthreads();
-    if (wave > 0)
-        return;
-    f4 gate = all[lane], up = all[64 + lane];
-    for (int w = 1; w < waves; ++w) {
-        gate += all[w * 128 + lane];
-        up += all[w * 128 + 64 + lane];
-    }
-    const int32_t ch = c0 + (lane >> 4) * 4;
-    if ((lane & 15) < tile.rows && ch < a.inner) {
-        f4 h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            h[i] = gated<true>(gate[i], up[i]);
-        store4(a.h, kF32, static_cast<int64_t>(tile.row + (lane & 15)) * a.inner + ch, h, a.inner - ch, a.inner % 4 == 0);
-    }
-}
-
-// Second products of up to 16 rows of one expert, given as codes: 16 channels;
-// results by place in 32 bits.
-template <int U>
-__global__ void __launch_bounds__(512) down_rows(ExpertArgs a, int32_t columns) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int waves = blockDim.x >> 6;
-    RowTile tile;
-    int32_t column;
-    if (!find_tile(a.offsets, a.experts, 16, columns, lane, &tile, &column))
-        return;
-    const int32_t c0 = column * 16;
-    const int64_t pitch = static_cast<int64_t>(a.ib) * kBlock;
-    const uint8_t *w = a.w2 + (static_cast<int64_t>(tile.expert) * a.hidden + min(c0 + (lane & 15), a.hidden - 1)) * pitch;
-    const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + c0 / kBlock) * a.ib;
-    const int32_t place = tile.row + min(lane & 15, tile.rows - 1);
-    f4 acc[1] = {};
-    for (int32_t b0 = wave; b0 < a.ib; b0 += waves * U) {
-        i8 wf[U];
-        RowPart xp[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = min(b0 + u * waves, a.ib - 1);
-            wf[u] = weight_part(w, b, lane);
-            xp[u] = row_codes(a.hq + place * pitch, a.hs + static_cast<int64_t>(b) * a.pairs + place, b, lane);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = b0 + u * waves;
-            if (b >= a.ib)
-                break;
-            const f4 p = mfma128(halves(wf[u]), halves(xp[u].code));
-            const float s = xp[u].scale * uniform_load(ws + b);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                acc[0][i] = fmaf(s, p[i], acc[0][i]);
-        }
-    }
-    sum_waves<1>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int, f4 sum) {
-        const int32_t ch = c0 + (lane >> 4) * 4;
-        if ((lane & 15) < tile.rows && ch < a.hidden)
-            store4(a.z, kF32, static_cast<int64_t>(place) * a.hidden + ch, sum, a.hidden - ch, a.hidden % 4 == 0);
-    });
-}
-
-// Single tokens: one row of x has no use for matrix instructions, and whole rows
-// of W are read in whole lines: a lane takes 16 of 1024 neighbouring channels, 8
-// lanes a block.
+// Single tokens.  What bounds them is the weights' bytes, and a compute unit takes
+// in no more than its share of the card's rate (some 20 GB/s: what it can have
+// outstanding, over the memory's latency), so the weights are spread evenly over
+// all of them: workgroups of 8 channels.  (Workgroups of 128 channels, which
+// could convert the inner rows to codes themselves, took 24 instead of 10 us for
+// the first products of 6 x 4 MB.)  One row of x has no use for matrix
+// instructions, and rows of W are read in whole lines: a lane takes 16 of 1024
+// neighbouring channels, 8 lanes a block.  Sort and weighted sum fall away.
 
 // The sum of 16 products of codes.
 __device__ __forceinline__ float dot16(const float *x, u4 w) {
@@ -746,12 +627,6 @@ hipError_t prepare(const ExpertArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Wavefronts that share `blocks` evenly: at most 8, and two blocks each before that many.
-int even_waves(int32_t blocks) {
-    const int32_t each = std::max((blocks + 7) / 8, std::min(blocks, 2));
-    return (blocks + each - 1) / each;
-}
-
 template <typename T>
 hipError_t gated_tokens(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
@@ -762,18 +637,17 @@ hipError_t gated_tokens(const ExpertArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-ExpertPath expert_path(int32_t n, int32_t k, int32_t experts, int32_t inner) {
+// One or two tokens of different experts: measured (bf16, 2048 x 1024 channels, 8 of 64
+// experts) 1 token 20.8 us, over tiles 27.6; 2 tokens 31.9 and 31.1; 4 tokens 57 and 39.
+bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner) {
     const int64_t pairs = static_cast<int64_t>(n) * k;
-    if (n <= 4 && pairs <= 64 && k * blocks_of(inner) <= 384)  // a token's inner rows in 50 KB of LDS
-        return ExpertPath::kTokens;
-    return pairs <= 16ll * experts ? ExpertPath::kFew : ExpertPath::kTiles;
+    return n <= 2 && pairs <= 64 && pairs <= experts && k * blocks_of(inner) <= 384;  // inner rows in 50 KB of LDS
 }
 
 hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
-    const ExpertPath path = expert_path(a.n, a.k, a.experts, a.inner);
     hipError_t e;
-    if (path == ExpertPath::kTokens) {
+    if (experts_by_token(a.n, a.k, a.experts, a.inner)) {
         e = a.type == kF32   ? gated_tokens<float>(a, stream)
             : a.type == kF16 ? gated_tokens<_Float16>(a, stream)
                              : gated_tokens<__bf16>(a, stream);
@@ -786,50 +660,40 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
     e = a.type == kF32 ? prepare<float>(a, stream) : a.type == kF16 ? prepare<_Float16>(a, stream) : prepare<__bf16>(a, stream);
     if (e != hipSuccess)
         return e;
-    if (path == ExpertPath::kFew) {
-        const int64_t tiles = most_tiles(a, 16);
-        const int32_t up = (a.inner + 15) / 16, down = (a.hidden + 15) / 16;
-        int waves = even_waves(a.hb);
-        gated_rows<2><<<tile_grid(tiles, up), waves * 64, waves * 2048, stream>>>(a, up);
-        if ((e = hipGetLastError()) != hipSuccess ||
-            (e = launch_quantize_rows(a.h, kF32, a.inner, a.pairs, a.inner, a.hq, a.hs, stream)) != hipSuccess)
-            return e;
-        waves = even_waves(a.ib);
-        down_rows<2><<<tile_grid(tiles, down), waves * 64, waves * 1024, stream>>>(a, down);
-        e = hipGetLastError();
-    } else {
-        using Small = TileShape<256, 64, 2, 4>;
-        using Mid = TileShape<256, 128, 2, 4>;
-        using Big = TileShape<256, 256, 2, 4>;
-        const int64_t each = a.pairs / a.experts;
-        // The inner rows are rounded to codes again, which turns an error of 4e-5 into one of
-        // 1.5e-3: below the rounding of bf16 results, not of others, whose first products are exact.
-        // The results' error is their own: exact products for 32 bits only.
-        if (a.type == kBf16)
-            e = each >= 192  ? gated_tiles<Big, false>(a, stream)
-                : each >= 96 ? gated_tiles<Mid, false>(a, stream)
-                             : gated_tiles<Small, false>(a, stream);
-        else
-            e = each >= 96 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
-        if (e != hipSuccess)
-            return e;
-        if (a.type == kF32)
-            e = each >= 192  ? down_tiles<Big, true, false>(a, stream)
-                : each >= 96 ? down_tiles<Mid, true, false>(a, stream)
-                             : down_tiles<Small, true, false>(a, stream);
-        else if (a.type == kF16)
-            e = each >= 192  ? down_tiles<Big, false, false>(a, stream)
-                : each >= 96 ? down_tiles<Mid, false, false>(a, stream)
-                             : down_tiles<Small, false, false>(a, stream);
-        else
-            e = each >= 192  ? down_tiles<Big, false, true>(a, stream)
-                : each >= 96 ? down_tiles<Mid, false, true>(a, stream)
-                             : down_tiles<Small, false, true>(a, stream);
-    }
+    // The tile's rows by the rows an expert has on average; a compute unit holds one tile of
+    // any of these (LDS), so the smaller ones are three blocks deep.  Measured (64 experts,
+    // bf16): 250 rows each 196 us, in tiles of 128 and 64 rows 226 and 251; 150 rows 151 us in
+    // 128, 175 in 256 and 64; 50 rows 111 in 64, 123 in 128.
+    using Small = TileShape<256, 64, 2, 4, 3>;
+    using Mid = TileShape<256, 128, 2, 4, 3>;
+    using Big = TileShape<256, 256, 2, 4>;
+    const int64_t each = a.pairs / a.experts;
+    // The inner rows are rounded to codes again, which turns an error of 4e-5 into one of
+    // 1.5e-3: below the rounding of bf16 results, not of others, whose first products are exact.
+    // The results' error is their own: exact products for 32 bits only.
+    if (a.type == kBf16)
+        e = each >= 192  ? gated_tiles<Big, false>(a, stream)
+            : each >= 96 ? gated_tiles<Mid, false>(a, stream)
+                         : gated_tiles<Small, false>(a, stream);
+    else
+        e = each >= 96 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
     if (e != hipSuccess)
         return e;
-    return path == ExpertPath::kTiles && a.type == kBf16 ? launch_combine<_Float16>(a, wide, stream)
-                                                         : launch_combine<float>(a, wide, stream);
+    if (a.type == kF32)
+        e = each >= 192  ? down_tiles<Big, true, false>(a, stream)
+            : each >= 96 ? down_tiles<Mid, true, false>(a, stream)
+                         : down_tiles<Small, true, false>(a, stream);
+    else if (a.type == kF16)
+        e = each >= 192  ? down_tiles<Big, false, false>(a, stream)
+            : each >= 96 ? down_tiles<Mid, false, false>(a, stream)
+                         : down_tiles<Small, false, false>(a, stream);
+    else
+        e = each >= 192  ? down_tiles<Big, false, true>(a, stream)
+            : each >= 96 ? down_tiles<Mid, false, true>(a, stream)
+                         : down_tiles<Small, false, true>(a, stream);
+    if (e != hipSuccess)
+        return e;
+    return a.type == kBf16 ? launch_combine<_Float16>(a, wide, stream) : launch_combine<float>(a, wide, stream);
 }
 
 }  // namespace spconv
