@@ -50,10 +50,12 @@ struct RouteArgs {
     int32_t groups, groups_kept, group_top;
     int32_t softmax, renorm;
     float factor;
-    // set by launch_route: experts of a group and its inverse, lanes that look through one
+    // set by launch_route: experts of a group and its inverse, lanes that look through one,
+    // whether those hold its experts
     int32_t each;
     uint32_t each_inverse;
     int32_t group_lanes;
+    bool whole_lanes;
 };
 constexpr int32_t kMostExperts = 1024;
 constexpr int32_t kMostChoices = 64;

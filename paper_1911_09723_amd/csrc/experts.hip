@@ -662,8 +662,8 @@ hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
         return e;
     // The tile's rows by the rows an expert has on average; a compute unit holds one tile of
     // any of these (LDS), so the smaller ones are three blocks deep.  Measured (64 experts,
-    // bf16): 250 rows each 196 us, in tiles of 128 and 64 rows 226 and 251; 150 rows 151 us in
-    // 128, 175 in 256 and 64; 50 rows 111 in 64, 123 in 128.
+    // bf16): 250 rows each 196 us, in tiles of 64 rows 251; 150 rows 151 us in tiles of 128, 175
+    // in 256 and in 64; 50 rows 111 in 64, 123 in 128.
     using Small = TileShape<256, 64, 2, 4, 3>;
     using Mid = TileShape<256, 128, 2, 4, 3>;
     using Big = TileShape<256, 256, 2, 4>;
