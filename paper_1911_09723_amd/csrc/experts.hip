@@ -394,27 +394,37 @@ constexpr int kTokenChannels = 2;  // gate and up channels of a wavefront
 template <typename T>
 __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t pair = blockIdx.y, e = a.ids[pair];
-    if (e < 0 || e >= a.experts)
-        return;
-    const int32_t c0 = (static_cast<int32_t>(blockIdx.x) * 4 + wave) * kTokenChannels;
+    const int32_t pair = blockIdx.y, c0 = (static_cast<int32_t>(blockIdx.x) * 4 + wave) * kTokenChannels;
     if (c0 >= a.inner)
         return;
     const int32_t pitch = a.hb * kBlock;
     const T *x = static_cast<const T *>(a.x) + (pair / a.k) * a.ldx;
+    constexpr int U = 2;
+    float v[U][16];
+    auto load_x = [&](int32_t k0) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int32_t k = k0 + j * 1024;
+            load8_tail(x + k, k < pitch ? a.hidden - k : 0, wide, v[j]);
+            load8_tail(x + k + 8, k < pitch ? a.hidden - k - 8 : 0, wide, v[j] + 8);
+        }
+    };
+    load_x(lane * 16);  // asked for before the id, which the weights' addresses wait for
+    const int32_t id = a.ids[pair];
+    const bool some = id >= 0 && id < a.experts;  // else any expert's weights, and no result
+    const int64_t e = some ? id : 0;
     const uint8_t *row[2 * kTokenChannels];
 #pragma unroll
     for (int i = 0; i < kTokenChannels; ++i) {
-        row[i] = a.w13 + (static_cast<int64_t>(e) * 2 * a.inner + min(c0 + i, a.inner - 1)) * pitch;
+        row[i] = a.w13 + (e * 2 * a.inner + min(c0 + i, a.inner - 1)) * pitch;
         row[i + kTokenChannels] = row[i] + static_cast<int64_t>(a.inner) * pitch;
     }
-    const float *sg = a.s13 + (static_cast<int64_t>(e) * 2 * a.ib + c0 / kBlock) * a.hb;
+    const float *sg = a.s13 + (e * 2 * a.ib + c0 / kBlock) * a.hb;
     const float *su = sg + static_cast<int64_t>(a.ib) * a.hb;
     float acc[2 * kTokenChannels] = {};
-    constexpr int U = 2;
-    for (int32_t k0 = lane * 16; k0 < pitch; k0 += U * 1024) {
+    for (int32_t k0 = lane * 16;;) {
         u4 w[U][2 * kTokenChannels];
-        float g[U], u[U], v[U][16];
+        float g[U], u[U];
         // a lane past the last channel repeats the last block's, times 0
 #pragma unroll
         for (int j = 0; j < U; ++j) {
@@ -425,12 +435,6 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
             const bool there = k0 + j * 1024 < pitch;
             g[j] = there ? sg[k / kBlock] : 0.0f;
             u[j] = there ? su[k / kBlock] : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const int32_t k = k0 + j * 1024;
-            load8_tail(x + k, k < pitch ? a.hidden - k : 0, wide, v[j]);
-            load8_tail(x + k + 8, k < pitch ? a.hidden - k - 8 : 0, wide, v[j] + 8);
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
@@ -447,11 +451,15 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
                 acc[i + kTokenChannels] = fmaf(dot16(v[j], w[j][i + kTokenChannels]), s.scale * u[j], acc[i + kTokenChannels]);
             }
         }
+        k0 += U * 1024;
+        if (k0 - lane * 16 >= pitch)
+            break;
+        load_x(k0);
     }
 #pragma unroll
     for (int i = 0; i < kTokenChannels; ++i) {
         const float h = gated<true>(sum_lanes(acc[i]), sum_lanes(acc[i + kTokenChannels]));
-        if (lane == 0 && c0 + i < a.inner)
+        if (lane == 0 && some && c0 + i < a.inner)
             a.h[static_cast<int64_t>(pair) * a.inner + c0 + i] = h;
     }
 }
@@ -482,14 +490,23 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
             s[u] = there ? a.s2[(of * a.hb + ch / kBlock) * a.ib + at / kBlock] * weights[j] : 0.0f;
         }
     };
-    load(0);
-    const int l = threadIdx.x & 15;
-    for (int32_t i = threadIdx.x >> 4; i < a.k * a.ib; i += 512 / 16) {
+    // inner rows to codes, 8 values a thread; the first are asked for before the ids, which
+    // the weights' addresses wait for.  Rows of ids that are no expert's were not written: zeros.
+    const int l = threadIdx.x & 15, groups = 512 / 16, blocks = a.k * a.ib;
+    float v[8];
+    auto load_h = [&](int32_t i) {
         const int32_t j = i / a.ib, c = (i - j * a.ib) * kBlock + 8 * l;
-        float v[8];
-        // rows of ids that are no expert's were not written: zeros
+        load8_tail(a.h + (static_cast<int64_t>(token) * a.k + j) * a.inner + c, i < blocks ? a.inner - c : 0,
+                   a.inner % 4 == 0, v);
+    };
+    load_h(threadIdx.x >> 4);
+    load(0);
+    for (int32_t i = threadIdx.x >> 4; i < blocks; i += groups) {
+        const int32_t j = i / a.ib, c = (i - j * a.ib) * kBlock + 8 * l;
         const bool there = static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(a.experts);
-        load8_tail(a.h + (static_cast<int64_t>(token) * a.k + j) * a.inner + c, there ? a.inner - c : 0, a.inner % 4 == 0, v);
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+            v[n] = there ? v[n] : 0.0f;
         uint32_t m = most8(v);
 #pragma unroll
         for (int d = 1; d < 16; d *= 2)
@@ -498,6 +515,7 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
         *reinterpret_cast<u2 *>(lds + j * pitch + c) = u2{codes4(v, q.inv), codes4(v + 4, q.inv)};
         if (l == 0)
             scales[i] = q.scale;
+        load_h(i + groups);
     }
     __syncthreads();
     float acc = 0.0f;
