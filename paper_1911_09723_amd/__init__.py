@@ -3,8 +3,10 @@
 The work happens in ``libspconv.so`` (C ABI in include/spconv.h): a host
 planner packs CSR / 1x2 / 1x4 block-CSR weights (or converts dense masked
 ones), and hand-written gfx950 HIP kernels compute act(W X + b) on NCHW fp32
-or fp16 tensors, optionally with a depthwise 3x3 stage fused in front.  This package is
-the thin Python binding plus the in-tree build script.
+or fp16 tensors, optionally with a depthwise 3x3 stage fused in front.  Beside them
+stand the operators of a language model's expert layers (``experts.py``): dense
+products in 8 bits with a scale for each block of 128, a router and the chosen
+experts' networks.  This package is the thin Python binding plus the in-tree build script.
 """
 
 from .spconv import (  # noqa: F401
@@ -47,6 +49,7 @@ from .spconv import (  # noqa: F401
     spconv_run,
 )
 from .experts import (  # noqa: F401
+    ExpertLayer,
     Experts,
     Fp8Linear,
     quantize_fp8,

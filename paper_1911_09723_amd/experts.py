@@ -16,7 +16,7 @@ from __future__ import annotations
 from functools import lru_cache
 
 from .spconv import (_ACTS, _SCORES, BF16, F16, F32, FP8, _check, _stream, load_library,
-                     spconv_experts_fp8_workspace, spconv_linear_fp8_workspace)
+                     spconv_experts_fp8_workspace, spconv_linear, spconv_linear_fp8_workspace)
 
 BLOCK = 128
 _TYPES = {}
@@ -51,11 +51,23 @@ def _current_device() -> int:
     return torch.cuda.current_device()
 
 
+def _gpu_of(t, what: str):
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % what)
+    return t.device
+
+
 def _given(t, shape, dtype, device, what: str):
     """t, checked to be a contiguous tensor of this shape and type on this device."""
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
     return t
+
+
+def _bytes(workspace, device) -> int:
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % device)
+    return workspace.numel() * workspace.element_size()
 
 
 def _blocks(n: int) -> int:
@@ -95,10 +107,10 @@ class Fp8Linear:
         import torch
         if act not in ("none", "relu", "relu6"):
             raise ValueError("act must be 'none', 'relu' or 'relu6'")
-        kb = _blocks(cin)
-        self.w = _given(w, (cout, kb * BLOCK), torch.float8_e4m3fn, w.device, "w")
-        self.w_scale = _given(w_scale, (_blocks(cout), kb), torch.float32, w.device, "w_scale")
-        self.bias = None if bias is None else _given(bias, (cout,), torch.float32, w.device, "bias")
+        kb, dev = _blocks(cin), _gpu_of(w, "w")
+        self.w = _given(w, (cout, kb * BLOCK), torch.float8_e4m3fn, dev, "w")
+        self.w_scale = _given(w_scale, (_blocks(cout), kb), torch.float32, dev, "w_scale")
+        self.bias = None if bias is None else _given(bias, (cout,), torch.float32, dev, "bias")
         self.cout, self.cin, self.act = int(cout), int(cin), act
 
     @classmethod
@@ -124,6 +136,8 @@ class Fp8Linear:
             dtype = dtype or (x.dtype if y is None else y.dtype)
         else:
             n, kind, ld = int(x.shape[0]), FP8, 0
+            if dev.index != _current_device():
+                raise ValueError("the layer must be on the current GPU")
             _given(x, (n, _blocks(self.cin) * BLOCK), torch.float8_e4m3fn, dev, "x")
             _given(x_scale, (_blocks(self.cin), n), torch.float32, dev, "x_scale")
             if dtype is None and y is None:
@@ -137,13 +151,13 @@ class Fp8Linear:
         if size and workspace is None:
             workspace = x.new_empty(size, dtype=torch.uint8)
         elif size:
-            size = workspace.numel() * workspace.element_size()
+            size = _bytes(workspace, dev)
         if n:
             _check(load_library().spconv_linear_fp8(
                 x.data_ptr(), kind, ld, None if x_scale is None else x_scale.data_ptr(),
                 self.w.data_ptr(), self.w_scale.data_ptr(), None if self.bias is None else self.bias.data_ptr(),
-                _ACTS[self.act], y.data_ptr(), _type(y.dtype, "y"), n, self.cin, self.cout, workspace.data_ptr() if size else None, size,
-                _stream(stream)))
+                _ACTS[self.act], y.data_ptr(), _type(y.dtype, "y"), n, self.cin, self.cout,
+                workspace.data_ptr() if size else None, size, _stream(stream)))
         return y
 
 
@@ -181,7 +195,7 @@ class Experts:
 
     def __init__(self, w13, w13_scale, w2, w2_scale, hidden: int, inner: int):
         import torch
-        f8, f32, dev = torch.float8_e4m3fn, torch.float32, w13.device
+        f8, f32, dev = torch.float8_e4m3fn, torch.float32, _gpu_of(w13, "w13")
         hb, ib, e = _blocks(hidden), _blocks(inner), int(w13.shape[0])
         self.w13 = _given(w13, (e, 2, inner, hb * BLOCK), f8, dev, "w13")
         self.w13_scale = _given(w13_scale, (e, 2, ib, hb), f32, dev, "w13_scale")
@@ -233,9 +247,85 @@ class Experts:
             size = self.workspace_bytes(n, k)
             workspace = x.new_empty(size, dtype=torch.uint8)
         else:
-            size = workspace.numel() * workspace.element_size()
+            size = _bytes(workspace, dev)
         _check(load_library().spconv_experts_fp8(
             x.data_ptr(), kind, ld, ids.data_ptr(), weights.data_ptr(), self.w13.data_ptr(), self.w13_scale.data_ptr(),
             self.w2.data_ptr(), self.w2_scale.data_ptr(), y.data_ptr(), n, k, self.experts, self.hidden, self.inner,
             workspace.data_ptr(), size, _stream(stream)))
         return y
+
+
+class ExpertLayer:
+    """A mixture-of-experts layer for one batch size, as a model's forward pass
+    runs it: the router's logits (``spconv_linear``, fp32), ``route``, the chosen
+    ``Experts``, the residual sum and, where ``head`` is given, a dense 8-bit
+    layer on top.
+
+    ``router`` is the router's weight [experts, hidden] in float32; ``score``,
+    ``bias``, ``groups``, ... are route()'s.  Buffers are made once; every step is
+    queued on torch's current stream.  ``capture`` records the steps into one
+    graph (torch.cuda.CUDAGraph over HIP graphs) and ``replay`` launches it on
+    what ``x`` holds.
+    """
+
+    def __init__(self, router, experts: Experts, k: int, batch: int, dtype=None, head: Fp8Linear = None,
+                 residual: bool = True, score: str = "softmax", bias=None, groups: int = 1, groups_kept: int = 1,
+                 group_top: int = 1, renorm: bool = True, factor: float = 1.0):
+        import torch
+        dev, f32 = experts.w13.device, torch.float32
+        dtype = dtype or torch.bfloat16
+        _type(dtype, "dtype")
+        self.router = _given(router, (experts.experts, experts.hidden), f32, dev, "router")
+        if head is not None and head.cin != experts.hidden:
+            raise ValueError("head must take %d channels" % experts.hidden)
+        self.experts, self.head, self.k, self.residual = experts, head, int(k), residual
+        self.choice = dict(score=score, bias=bias, groups=groups, groups_kept=groups_kept, group_top=group_top,
+                           renorm=renorm, factor=factor)
+
+        def make(cols, kind):
+            return torch.zeros((batch, cols), dtype=kind, device=dev)
+
+        self.x = make(experts.hidden, dtype)  # the static input
+        self.x32 = make(experts.hidden, f32)
+        self.logits = make(experts.experts, f32)
+        self.ids, self.weights = make(k, torch.int32), make(k, f32)
+        self.y = make(experts.hidden, dtype)
+        self.out = self.y if head is None else make(head.cout, dtype)
+        self.space = torch.empty(experts.workspace_bytes(batch, k), dtype=torch.uint8, device=dev)
+        self.head_space = None if head is None else torch.empty(head.workspace_bytes(batch, dtype), dtype=torch.uint8,
+                                                                device=dev)
+        self.graph = None
+
+    def forward(self, x=None):
+        """Queue the layer (copying x into the static input first when given); returns the output buffer."""
+        if x is not None:
+            self.x.copy_(x)
+        e = self.experts
+        self.x32.copy_(self.x)
+        spconv_linear(self.x32, self.router, None, "none", self.logits, self.x.shape[0], e.hidden, e.experts)
+        route(self.logits, self.k, ids=self.ids, weights=self.weights, **self.choice)
+        e.run(self.x, self.ids, self.weights, self.y, self.space)
+        if self.residual:
+            self.y.add_(self.x)
+        if self.head is not None:
+            self.head.run(self.y, y=self.out, workspace=self.head_space)
+        return self.out
+
+    def capture(self):
+        """Record the steps into one graph (after one warm-up pass)."""
+        import torch
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.forward()
+        torch.cuda.current_stream().wait_stream(side)
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.forward()
+        return self.graph
+
+    def replay(self):
+        if self.graph is None:
+            raise RuntimeError("capture() first")
+        self.graph.replay()
+        return self.out
