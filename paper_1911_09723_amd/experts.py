@@ -15,21 +15,37 @@ from __future__ import annotations
 
 from functools import lru_cache
 
-from .spconv import (_ACTS, _SCORES, BF16, F16, F32, FP8, _check, _stream, load_library,
-                     spconv_experts_fp8_workspace, spconv_linear, spconv_linear_fp8_workspace)
+from .spconv import (_ACTS, _SCORES, BF16, F16, F32, FP8, _check, load_library, spconv_experts_fp8_workspace,
+                     spconv_linear, spconv_linear_fp8_workspace)
 
 BLOCK = 128
+# bound by _bind, at the first call that needs torch: a call's host time is that of its launch
+# (3.5 us) and what stands here, so nothing is looked up twice
+_torch = None
 _TYPES = {}
+_lib = _device = _raw_stream = None
 # sizes are asked for on every call
 _linear_workspace = lru_cache(maxsize=1024)(spconv_linear_fp8_workspace)
 _experts_workspace = lru_cache(maxsize=1024)(spconv_experts_fp8_workspace)
 
 
+def _bind():
+    global _torch, _lib, _device, _raw_stream
+    import torch
+    _lib = load_library()
+    _device = torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if _raw_stream is None:
+        def _raw_stream(device):
+            return torch.cuda.current_stream(device).cuda_stream
+    _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    _torch = torch
+
+
 def _type(dtype, what: str) -> int:
     """The library's number for a torch element type."""
-    if not _TYPES:
-        import torch
-        _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    if _torch is None:
+        _bind()
     try:
         return _TYPES[dtype]
     except KeyError:
@@ -37,18 +53,22 @@ def _type(dtype, what: str) -> int:
 
 
 def _matrix(x, what: str):
-    """(rows, cols, row stride) of a matrix on the current GPU whose rows are contiguous."""
-    if x.dim() != 2 or not x.is_cuda or x.get_device() != _current_device():
+    """(rows, cols, row stride, device) of a matrix on the current GPU whose rows are contiguous."""
+    device = x.get_device()
+    if device < 0 or x.dim() != 2 or device != _device():
         raise ValueError("%s must be a matrix on the current GPU" % what)
     rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    ld, step = x.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % what)
-    return rows, cols, x.stride(0) if rows > 1 else cols
+    return rows, cols, ld if rows > 1 else cols, device
 
 
-def _current_device() -> int:
-    import torch
-    return torch.cuda.current_device()
+def _handle(stream, device) -> int:
+    """The address of a torch stream, or of torch's current one on the device."""
+    if stream is None:
+        return _raw_stream(device)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _gpu_of(t, what: str):
@@ -59,8 +79,8 @@ def _gpu_of(t, what: str):
 
 def _given(t, shape, dtype, device, what: str):
     """t, checked to be a contiguous tensor of this shape and type on this device."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, shape, device))
     return t
 
 
@@ -78,24 +98,23 @@ def quantize_fp8(x, block_rows: int = 1, q=None, scale=None, stream=None):
     """A matrix [rows, cols] as 8-bit codes [rows, 128 kb] (float8_e4m3fn, kb =
     ceil(cols / 128)) and scales: [kb, rows] with block_rows = 1 (activations),
     [ceil(rows / 128), kb] with block_rows = 128 (weights)."""
-    import torch
     kind = _type(x.dtype, "x")
-    rows, cols, ld = _matrix(x, "x")
+    rows, cols, ld, device = _matrix(x, "x")
     if block_rows not in (1, BLOCK):
         raise ValueError("block_rows must be 1 or %d" % BLOCK)
-    kb = _blocks(cols)
-    shape, codes = (kb, rows) if block_rows == 1 else (_blocks(rows), kb), (rows, kb * BLOCK)
+    kb = -(-cols // BLOCK)
+    shape = (kb, rows) if block_rows == 1 else (-(-rows // BLOCK), kb)
     if q is None:
-        q = x.new_empty(codes, dtype=torch.float8_e4m3fn)
+        q = x.new_empty((rows, kb * BLOCK), dtype=_torch.float8_e4m3fn)
     else:
-        _given(q, codes, torch.float8_e4m3fn, x.device, "q")
+        _given(q, (rows, kb * BLOCK), _torch.float8_e4m3fn, x.device, "q")
     if scale is None:
-        scale = x.new_empty(shape, dtype=torch.float32)
+        scale = x.new_empty(shape, dtype=_torch.float32)
     else:
-        _given(scale, shape, torch.float32, x.device, "scale")
+        _given(scale, shape, _torch.float32, x.device, "scale")
     if rows and cols:
-        _check(load_library().spconv_quantize_fp8(x.data_ptr(), kind, ld, rows, cols, block_rows, q.data_ptr(),
-                                                  scale.data_ptr(), _stream(stream)))
+        _check(_lib.spconv_quantize_fp8(x.data_ptr(), kind, ld, rows, cols, block_rows, q.data_ptr(), scale.data_ptr(),
+                                        _handle(stream, device)))
     return q, scale
 
 
@@ -111,7 +130,7 @@ class Fp8Linear:
         self.w = _given(w, (cout, kb * BLOCK), torch.float8_e4m3fn, dev, "w")
         self.w_scale = _given(w_scale, (_blocks(cout), kb), torch.float32, dev, "w_scale")
         self.bias = None if bias is None else _given(bias, (cout,), torch.float32, dev, "bias")
-        self.cout, self.cin, self.act = int(cout), int(cin), act
+        self.cout, self.cin, self.act, self.device = int(cout), int(cin), act, dev
 
     @classmethod
     def from_dense(cls, weight, bias=None, act: str = "none"):
@@ -126,38 +145,40 @@ class Fp8Linear:
     def run(self, x, x_scale=None, y=None, dtype=None, workspace=None, stream=None):
         """y [n, cout] for x [n, cin], or for quantize_fp8's codes and scales
         (then ``dtype`` or ``y`` gives y's type; it is x's otherwise)."""
-        import torch
-        dev = self.w.device
         if x_scale is None:
             kind = _type(x.dtype, "x")
-            n, cols, ld = _matrix(x, "x")
-            if cols != self.cin or x.device != dev:
-                raise ValueError("x must have %d channels and be on %s" % (self.cin, dev))
+            n, cols, ld, device = _matrix(x, "x")
+            if cols != self.cin or device != self.device.index:
+                raise ValueError("x must have %d channels and be on %s" % (self.cin, self.device))
             dtype = dtype or (x.dtype if y is None else y.dtype)
         else:
-            n, kind, ld = int(x.shape[0]), FP8, 0
-            if dev.index != _current_device():
+            n, kind, ld, device = int(x.shape[0]), FP8, 0, self.device.index
+            if _torch is None:
+                _bind()
+            if device != _device():
                 raise ValueError("the layer must be on the current GPU")
-            _given(x, (n, _blocks(self.cin) * BLOCK), torch.float8_e4m3fn, dev, "x")
-            _given(x_scale, (_blocks(self.cin), n), torch.float32, dev, "x_scale")
+            _given(x, (n, _blocks(self.cin) * BLOCK), _torch.float8_e4m3fn, self.device, "x")
+            _given(x_scale, (_blocks(self.cin), n), _torch.float32, self.device, "x_scale")
             if dtype is None and y is None:
                 raise ValueError("quantised rows need y or its dtype")
             dtype = dtype or y.dtype
         if y is None:
             y = x.new_empty((n, self.cout), dtype=dtype)
         else:
-            _given(y, (n, self.cout), dtype, dev, "y")
+            _given(y, (n, self.cout), dtype, self.device, "y")
         size = _linear_workspace(kind, n, self.cin, self.cout)
-        if size and workspace is None:
-            workspace = x.new_empty(size, dtype=torch.uint8)
-        elif size:
-            size = _bytes(workspace, dev)
+        space = None
+        if size:
+            if workspace is None:
+                workspace = x.new_empty(size, dtype=_torch.uint8)
+            else:
+                size = _bytes(workspace, self.device)
+            space = workspace.data_ptr()
         if n:
-            _check(load_library().spconv_linear_fp8(
-                x.data_ptr(), kind, ld, None if x_scale is None else x_scale.data_ptr(),
-                self.w.data_ptr(), self.w_scale.data_ptr(), None if self.bias is None else self.bias.data_ptr(),
-                _ACTS[self.act], y.data_ptr(), _type(y.dtype, "y"), n, self.cin, self.cout,
-                workspace.data_ptr() if size else None, size, _stream(stream)))
+            _check(_lib.spconv_linear_fp8(
+                x.data_ptr(), kind, ld, None if x_scale is None else x_scale.data_ptr(), self.w.data_ptr(),
+                self.w_scale.data_ptr(), None if self.bias is None else self.bias.data_ptr(), _ACTS[self.act],
+                y.data_ptr(), _type(dtype, "y"), n, self.cin, self.cout, space, size, _handle(stream, device)))
         return y
 
 
@@ -166,24 +187,23 @@ def route(logits, k: int, score: str = "softmax", bias=None, groups: int = 1, gr
     """The k experts (int32) of each token and their weights (float32), both
     [n, k], from a router's logits [n, experts]; spconv_route in
     include/spconv.h defines them."""
-    import torch
     kind = _type(logits.dtype, "logits")
-    n, experts, ld = _matrix(logits, "logits")
-    if score not in ("softmax", "sigmoid"):
+    n, experts, ld, device = _matrix(logits, "logits")
+    if score not in _SCORES:
         raise ValueError("score must be 'softmax' or 'sigmoid'")
     if bias is not None:
-        _given(bias, (experts,), torch.float32, logits.device, "bias")
+        _given(bias, (experts,), _torch.float32, logits.device, "bias")
     if ids is None:
-        ids = logits.new_empty((n, max(k, 0)), dtype=torch.int32)
+        ids = logits.new_empty((n, max(k, 0)), dtype=_torch.int32)
     else:
-        _given(ids, (n, k), torch.int32, logits.device, "ids")
+        _given(ids, (n, k), _torch.int32, logits.device, "ids")
     if weights is None:
-        weights = logits.new_empty((n, max(k, 0)), dtype=torch.float32)
+        weights = logits.new_empty((n, max(k, 0)), dtype=_torch.float32)
     else:
-        _given(weights, (n, k), torch.float32, logits.device, "weights")
-    _check(load_library().spconv_route(
-        logits.data_ptr(), kind, ld, None if bias is None else bias.data_ptr(), _SCORES[score], n, experts, groups,
-        groups_kept, group_top, k, renorm, factor, ids.data_ptr(), weights.data_ptr(), _stream(stream)))
+        _given(weights, (n, k), _torch.float32, logits.device, "weights")
+    _check(_lib.spconv_route(logits.data_ptr(), kind, ld, None if bias is None else bias.data_ptr(), _SCORES[score], n,
+                             experts, groups, groups_kept, group_top, k, renorm, factor, ids.data_ptr(),
+                             weights.data_ptr(), _handle(stream, device)))
     return ids, weights
 
 
@@ -201,7 +221,7 @@ class Experts:
         self.w13_scale = _given(w13_scale, (e, 2, ib, hb), f32, dev, "w13_scale")
         self.w2 = _given(w2, (e, hidden, ib * BLOCK), f8, dev, "w2")
         self.w2_scale = _given(w2_scale, (e, hb, ib), f32, dev, "w2_scale")
-        self.experts, self.hidden, self.inner = e, int(hidden), int(inner)
+        self.experts, self.hidden, self.inner, self.device = e, int(hidden), int(inner), dev
 
     @classmethod
     def from_dense(cls, w1, w3, w2):
@@ -228,30 +248,28 @@ class Experts:
     def run(self, x, ids, weights, y=None, workspace=None, stream=None):
         """y [n, hidden] = the sum of the experts' outputs for x [n, hidden],
         with ids (int32) and weights (float32) [n, k] as route() gives them."""
-        import torch
-        dev = self.w13.device
         kind = _type(x.dtype, "x")
-        n, cols, ld = _matrix(x, "x")
-        if cols != self.hidden or x.device != dev:
-            raise ValueError("x must have %d channels and be on %s" % (self.hidden, dev))
+        n, cols, ld, device = _matrix(x, "x")
+        if cols != self.hidden or device != self.device.index:
+            raise ValueError("x must have %d channels and be on %s" % (self.hidden, self.device))
         if ids.dim() != 2:
             raise ValueError("ids must be a matrix [n, k]")
-        k = int(ids.shape[1])
-        _given(ids, (n, k), torch.int32, dev, "ids")
-        _given(weights, (n, k), torch.float32, dev, "weights")
+        k = ids.shape[1]
+        _given(ids, (n, k), _torch.int32, self.device, "ids")
+        _given(weights, (n, k), _torch.float32, self.device, "weights")
         if y is None:
             y = x.new_empty((n, cols))
         else:
-            _given(y, (n, cols), x.dtype, dev, "y")
+            _given(y, (n, cols), x.dtype, self.device, "y")
         if workspace is None:
             size = self.workspace_bytes(n, k)
-            workspace = x.new_empty(size, dtype=torch.uint8)
+            workspace = x.new_empty(size, dtype=_torch.uint8)
         else:
-            size = _bytes(workspace, dev)
-        _check(load_library().spconv_experts_fp8(
+            size = _bytes(workspace, self.device)
+        _check(_lib.spconv_experts_fp8(
             x.data_ptr(), kind, ld, ids.data_ptr(), weights.data_ptr(), self.w13.data_ptr(), self.w13_scale.data_ptr(),
             self.w2.data_ptr(), self.w2_scale.data_ptr(), y.data_ptr(), n, k, self.experts, self.hidden, self.inner,
-            workspace.data_ptr(), size, _stream(stream)))
+            workspace.data_ptr(), size, _handle(stream, device)))
         return y
 
 
