@@ -73,7 +73,7 @@ struct ExpertArgs {
     int32_t type;              // of x and y
     int32_t n, k, pairs, experts, hidden, inner;
     int32_t hb, ib;            // blocks of 128 hidden and inner channels
-    // workspace: the pairs sorted by expert (order[place] = pair, place[pair], -1 where
+    // workspace: the pairs sorted by expert (order[place] = token, place[pair], -1 where
     // the id is no expert, offsets[experts + 1] = each expert's first place), x's codes,
     // the inner rows' codes and the results by place; token by token only the inner rows,
     // in 32 bits by pair (h)

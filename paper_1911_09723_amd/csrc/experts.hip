@@ -92,7 +92,7 @@ __device__ __forceinline__ void sort_pairs(const ExpertArgs &a, int32_t e, bool 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (v[j] == e) {
-                a.order[before] = i + j;
+                a.order[before] = (i + j) / a.k;
                 a.place[i + j] = before++;
             } else if (e == 0 && i + j < a.pairs && static_cast<uint32_t>(v[j]) >= static_cast<uint32_t>(a.experts)) {
                 a.place[i + j] = -1;
@@ -218,17 +218,19 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        if (line < S::BC) {  // lines of a wavefront: 64 gate, then 64 up channels
+        if (i < S::kWeightLoads) {  // lines of a wavefront: 64 gate, then 64 up channels
             const int32_t ch = fb * kBlock + line / 128 * 64 + line % 64;
-            from.at[i] = ch < a.inner ? (ch + (line & 64 ? a.inner : 0)) * pitch + tile_byte(line, lane) : from.w_bytes;
+            const uint32_t at = (ch + (line & 64 ? a.inner : 0)) * pitch + tile_byte(line, lane);
+            from.at[i] = ch < a.inner ? at : from.w_bytes;
         } else {
             const int r = line - S::BC;
-            from.at[i] = r < tile.rows ? a.order[tile.row + r] / a.k * pitch + tile_byte(line, lane) : from.x_bytes;
+            const uint32_t at = a.order[tile.row + min(r, tile.rows - 1)] * pitch + tile_byte(line, lane);
+            from.at[i] = r < tile.rows ? at : from.x_bytes;
         }
     }
     from.rows = tile.rows;
     from.xs = a.xs;
-    from.xs_at = a.order[tile.row + min(wave % (S::BT / 64) * 64 + lane, tile.rows - 1)] / a.k * 4u;
+    from.xs_at = a.order[tile.row + min(wave % (S::BT / 64) * 64 + lane, tile.rows - 1)] * 4u;
     from.xs_step = a.n * 4u;
     from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
@@ -310,7 +312,7 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
-        if (line < S::BC)
+        if (i < S::kWeightLoads)
             from.at[i] = line < a.hidden - c0 ? line * pitch + tile_byte(line, lane) : from.w_bytes;
         else
             from.at[i] = line - S::BC < tile.rows ? (line - S::BC) * pitch + tile_byte(line, lane) : from.x_bytes;
