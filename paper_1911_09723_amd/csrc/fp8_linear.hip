@@ -82,33 +82,26 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
 }
 
 // XT: Fp8 (codes) or the type of rows that are quantised here.
-template <typename XT, int TT, int CT, int U>
+template <typename XT, int TT, int U>
 __global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x, bool wide) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    const int32_t c0 = blockIdx.x * 16 * CT, t0 = blockIdx.y * 16 * TT;
+    const int32_t c0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * TT;
     const int64_t pitch = static_cast<int64_t>(a.kb) * kBlock;
-    const uint8_t *w[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-        w[c] = a.w + min(c0 + c * 16 + (lane & 15), a.cout - 1) * pitch;
+    const uint8_t *w = a.w + min(c0 + (lane & 15), a.cout - 1) * pitch;
     const float *ws = a.ws + static_cast<int64_t>(c0 / kBlock) * a.kb;
     int32_t row[TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
         row[t] = min(t0 + t * 16 + (lane & 15), a.n - 1);
-    f4 acc[CT * TT] = {};
+    f4 acc[TT] = {};
     for (int32_t b0 = wave; b0 < a.kb; b0 += waves * U) {
-        i8 wf[U][CT];
+        i8 wf[U];
         RowPart xp[U][TT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t b = min(b0 + u * waves, a.kb - 1);
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                wf[u][c] = weight_part(w[c], b, lane);
-        }
+        for (int u = 0; u < U; ++u)
+            wf[u] = weight_part(w, min(b0 + u * waves, a.kb - 1), lane);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t b = min(b0 + u * waves, a.kb - 1);
@@ -126,43 +119,36 @@ __global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x,
             if (b0 + u * waves >= a.kb)
                 break;
             const float sw = ws[b0 + u * waves];
-            Halves wh[CT];
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-                wh[c] = halves(wf[u][c]);
+            const Halves wh = halves(wf[u]);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
-                const Halves xh = halves(xp[u][t].code);
                 const float s = xp[u][t].scale * sw;
+                const f4 p = mfma128(wh, halves(xp[u][t].code));
 #pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const f4 p = mfma128(wh[c], xh);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        acc[c * TT + t][i] = fmaf(s, p[i], acc[c * TT + t][i]);
-                }
+                for (int i = 0; i < 4; ++i)
+                    acc[t][i] = fmaf(s, p[i], acc[t][i]);
             }
         }
     }
-    sum_waves<CT * TT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int i, f4 sum) {
-        finish(a, wide, t0 + i % TT * 16 + (lane & 15), c0 + i / TT * 16 + (lane >> 4) * 4, sum);
+    sum_waves<TT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int i, f4 sum) {
+        finish(a, wide, t0 + i * 16 + (lane & 15), c0 + (lane >> 4) * 4, sum);
     });
 }
 
-constexpr int32_t kStreamRows = 32;     // most rows that take the stream kernel
-constexpr int32_t kStreamQuantize = 16; // most rows that it quantises itself
+constexpr int32_t kStreamRows = 32;  // most rows that take the stream kernel
+constexpr int kStreamWaves = 16;
 
 size_t size_of(int32_t type) { return type == kF32 ? 4 : type == kFp8 ? 1 : 2; }
 
 template <typename XT, int TT>
 hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_t stream) {
-    const int waves = std::min(a.kb, 16);
+    const int waves = std::min(a.kb, kStreamWaves);
     const dim3 grid((a.cout + 15) / 16, (a.n + 16 * TT - 1) / (16 * TT));
     const size_t lds = static_cast<size_t>(waves) * TT * 1024;
     if (a.kb > waves)
-        linear_stream<XT, TT, 1, 2><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+        linear_stream<XT, TT, 2><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
     else
-        linear_stream<XT, TT, 1, 1><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+        linear_stream<XT, TT, 1><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
     return hipGetLastError();
 }
 
@@ -181,7 +167,16 @@ hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream) {
 
 }  // namespace
 
-bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) { return n <= kStreamQuantize; }
+// The stream kernel quantises its rows itself, which saves a launch, but does so in every
+// workgroup: a wavefront's blocks times a compute unit's workgroups are how often it waits for a
+// conversion.  Measured (bf16, two launches in brackets): once, 1 x 1024 -> 1024 3.8 us (5.1); twice,
+// 1 x 4096 -> 4096 8.9 (8.2), 1 x 1024 -> 8192 5.0 (5.7), 32 x 4096 -> 2048 9.7 (10.4), and the
+// second launch costs the host 3.5; four times, 1 x 8192 -> 1024 13.3 (10.2), 32 x 1024 -> 8192 8.7
+// (7.5), 24 x 4096 -> 4096 18.3 (10.8).
+bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) {
+    const int64_t groups = static_cast<int64_t>((cout + 15) / 16) * ((n + 15) / 16);
+    return n <= kStreamRows && (blocks_of(cin) + kStreamWaves - 1) / kStreamWaves * ((groups + 255) / 256) <= 2;
+}
 
 // Which kernel.  Up to 32 rows the stream kernel: the weight's bytes bound it (24 x 4096 ->
 // 4096: 8.7 us, the smallest tiles 11.5; 64 rows 14.5 and 11.5).  Then tiles, the largest that
