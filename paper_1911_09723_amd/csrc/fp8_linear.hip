@@ -82,26 +82,33 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
 }
 
 // XT: Fp8 (codes) or the type of rows that are quantised here.
-template <typename XT, int TT, int U>
+template <typename XT, int TT, int CT, int U>
 __global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x, bool wide) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    const int32_t c0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * TT;
+    const int32_t c0 = blockIdx.x * 16 * CT, t0 = blockIdx.y * 16 * TT;
     const int64_t pitch = static_cast<int64_t>(a.kb) * kBlock;
-    const uint8_t *w = a.w + min(c0 + (lane & 15), a.cout - 1) * pitch;
+    const uint8_t *w[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+        w[c] = a.w + min(c0 + c * 16 + (lane & 15), a.cout - 1) * pitch;
     const float *ws = a.ws + static_cast<int64_t>(c0 / kBlock) * a.kb;
     int32_t row[TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
         row[t] = min(t0 + t * 16 + (lane & 15), a.n - 1);
-    f4 acc[TT] = {};
+    f4 acc[CT * TT] = {};
     for (int32_t b0 = wave; b0 < a.kb; b0 += waves * U) {
-        i8 wf[U];
+        i8 wf[U][CT];
         RowPart xp[U][TT];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            wf[u] = weight_part(w, min(b0 + u * waves, a.kb - 1), lane);
+        for (int u = 0; u < U; ++u) {
+            const int32_t b = min(b0 + u * waves, a.kb - 1);
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                wf[u][c] = weight_part(w[c], b, lane);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t b = min(b0 + u * waves, a.kb - 1);
@@ -119,19 +126,26 @@ __global__ void __launch_bounds__(1024) linear_stream(LinearArgs a, bool wide_x,
             if (b0 + u * waves >= a.kb)
                 break;
             const float sw = ws[b0 + u * waves];
-            const Halves wh = halves(wf[u]);
+            Halves wh[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                wh[c] = halves(wf[u][c]);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
+                const Halves xh = halves(xp[u][t].code);
                 const float s = xp[u][t].scale * sw;
-                const f4 p = mfma128(wh, halves(xp[u][t].code));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc[t][i] = fmaf(s, p[i], acc[t][i]);
+                for (int c = 0; c < CT; ++c) {
+                    const f4 p = mfma128(wh[c], xh);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[c * TT + t][i] = fmaf(s, p[i], acc[c * TT + t][i]);
+                }
             }
         }
     }
-    sum_waves<TT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int i, f4 sum) {
-        finish(a, wide, t0 + i * 16 + (lane & 15), c0 + (lane >> 4) * 4, sum);
+    sum_waves<CT * TT>(acc, reinterpret_cast<f4 *>(lds), waves, wave, lane, [&](int i, f4 sum) {
+        finish(a, wide, t0 + i % TT * 16 + (lane & 15), c0 + i / TT * 16 + (lane >> 4) * 4, sum);
     });
 }
 
@@ -140,15 +154,15 @@ constexpr int kStreamWaves = 16;
 
 size_t size_of(int32_t type) { return type == kF32 ? 4 : type == kFp8 ? 1 : 2; }
 
-template <typename XT, int TT>
+template <typename XT, int TT, int CT>
 hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_t stream) {
     const int waves = std::min(a.kb, kStreamWaves);
-    const dim3 grid((a.cout + 15) / 16, (a.n + 16 * TT - 1) / (16 * TT));
-    const size_t lds = static_cast<size_t>(waves) * TT * 1024;
+    const dim3 grid((a.cout + 16 * CT - 1) / (16 * CT), (a.n + 16 * TT - 1) / (16 * TT));
+    const size_t lds = static_cast<size_t>(waves) * CT * TT * 1024;
     if (a.kb > waves)
-        linear_stream<XT, TT, 2><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+        linear_stream<XT, TT, CT, 2><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
     else
-        linear_stream<XT, TT, 1><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
+        linear_stream<XT, TT, CT, 1><<<grid, waves * 64, lds, stream>>>(a, wide_x, wide);
     return hipGetLastError();
 }
 
@@ -179,7 +193,10 @@ bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) {
 }
 
 // Which kernel.  Up to 32 rows the stream kernel: the weight's bytes bound it (24 x 4096 ->
-// 4096: 8.7 us, the smallest tiles 11.5; 64 rows 14.5 and 11.5).  Then tiles, the largest that
+// 4096: 8.7 us, the smallest tiles 11.5; 64 rows 14.5 and 11.5).  Each of its workgroups reads all
+// rows, as many bytes as of the weight at 16 rows: 32 channels a workgroup in place of 16 where
+// that still gives every compute unit one (with the rows' conversion, 32 x 8192 -> 8192: 31.4 to
+// 24.5 us, 16 x 4096 -> 8192 12.5 to 11.1; 32 x 8192 -> 4096 17.8 and 22.0).  Then tiles, the largest that
 // still give the card's 256 compute units work: a tile of 64 x 64 four blocks deep where there
 // are no more of those than compute units (128 rows of 4096 -> 4096: 11.7 us against 15.2 in
 // tiles of 128 x 64), 256 x 256 from 112 on (2048 rows: 47.8 against 52.1; 1536: 39.4 against 39.0
@@ -191,13 +208,14 @@ hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
     const bool wide_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size_of(a.x_type) % 16 == 0;
     const bool wide = a.cout % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
     if (a.x_type != kFp8)
-        return a.x_type == kF32   ? stream_launch<float, 1>(a, wide_x, wide, stream)
-               : a.x_type == kF16 ? stream_launch<_Float16, 1>(a, wide_x, wide, stream)
-                                  : stream_launch<__bf16, 1>(a, wide_x, wide, stream);
+        return a.x_type == kF32   ? stream_launch<float, 1, 1>(a, wide_x, wide, stream)
+               : a.x_type == kF16 ? stream_launch<_Float16, 1, 1>(a, wide_x, wide, stream)
+                                  : stream_launch<__bf16, 1, 1>(a, wide_x, wide, stream);
+    const bool pairs = a.n > 8 && a.cout >= 8192;
     if (a.n <= 16)
-        return stream_launch<Fp8, 1>(a, wide_x, wide, stream);
+        return pairs ? stream_launch<Fp8, 1, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 1, 1>(a, wide_x, wide, stream);
     if (a.n <= kStreamRows)
-        return stream_launch<Fp8, 2>(a, wide_x, wide, stream);
+        return pairs ? stream_launch<Fp8, 2, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 2, 1>(a, wide_x, wide, stream);
     auto tiles = [&](int32_t channels, int32_t rows) {
         return static_cast<int64_t>((a.cout + channels - 1) / channels) * ((a.n + rows - 1) / rows);
     };

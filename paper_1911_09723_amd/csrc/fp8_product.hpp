@@ -313,8 +313,8 @@ __device__ __forceinline__ void store_tile(const f4 (&acc)[S::NC][S::NT], void *
 }
 
 // ---------------------------------------------------------------------------
-// Stream core: up to 16 TT rows against 16 channels, the blocks of the input
-// channels dealt to the wavefronts of a workgroup in turn.
+// Stream core: up to 16 TT rows against CT pieces of 16 channels, the blocks
+// of the input channels dealt to the wavefronts of a workgroup in turn.
 // Nothing is shared between wavefronts but the final sum, so operands go from
 // global memory (rows: from L2) to registers in the instruction's layout.  What
 // bounds it is the weight's bytes, so the products are the exact ones.

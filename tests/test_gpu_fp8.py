@@ -113,6 +113,18 @@ def test_linear_many_rows_or_channels(dtype, n, cin, cout):
     _check_linear(layer.run(x), x, layer, b, "none", dtype)
 
 
+# few rows: quantised in the product or before it, one or two pieces of channels a workgroup
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,cin,cout", [(1, 2100, 8211), (9, 2100, 8211), (17, 4500, 8211), (32, 640, 8200),
+                                        (3, 8100, 70), (20, 4224, 300), (32, 900, 2050), (8, 2049, 8190)])
+def test_linear_few_rows(dtype, n, cin, cout):
+    note("linear %s n %d cin %d cout %d" % (dtype, n, cin, cout))
+    w, b = _layer(cout, cin, 5, True)
+    layer = sp.Fp8Linear.from_dense(w, b)
+    x = _rows(n, cin, dtype, 6, 1)
+    _check_linear(layer.run(x), x, layer, b, "none", dtype)
+
+
 @pytest.mark.parametrize("n", [1, 16, 17, 40, 64, 65, 300])
 @pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
 def test_linear_of_quantised_rows(n, out):
