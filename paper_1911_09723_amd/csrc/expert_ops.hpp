@@ -82,11 +82,12 @@ struct ExpertArgs {
     float *xs, *hs, *h;
     void *z;    // f32, or f16 with scales zs [pairs][hb]
     float *zs;
+    uint32_t k_inverse;  // set by launch_experts: above 2^31 / k by at most 1
 };
 
 // Whether a call runs token by token, each pair reading its expert's weights, instead of
 // over tiles of the rows of one expert.
 bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner);
-hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream);
+hipError_t launch_experts(ExpertArgs a, hipStream_t stream);
 
 }  // namespace spconv

@@ -14,6 +14,11 @@ namespace {
 
 constexpr int kXcds = 8;
 
+// pair / k, for pairs below 2^25 and k up to 64.
+__device__ __forceinline__ int32_t token_of(const ExpertArgs &a, int32_t pair) {
+    return static_cast<int32_t>(static_cast<uint64_t>(pair) * a.k_inverse >> 31);
+}
+
 // Pairs (token, choice) sorted by expert: workgroup e finds the places of expert
 // e's pairs.  It counts, over all pairs, those of lower experts (its first place)
 // and its own, then hands out its places in the order of the pairs; no workgroup
@@ -92,7 +97,7 @@ __device__ __forceinline__ void sort_pairs(const ExpertArgs &a, int32_t e, bool 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (v[j] == e) {
-                a.order[before] = (i + j) / a.k;
+                a.order[before] = token_of(a, i + j);
                 a.place[i + j] = before++;
             } else if (e == 0 && i + j < a.pairs && static_cast<uint32_t>(v[j]) >= static_cast<uint32_t>(a.experts)) {
                 a.place[i + j] = -1;
@@ -664,7 +669,8 @@ bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner) {
     return n <= 2 && pairs <= 64 && pairs <= experts && k * blocks_of(inner) <= 384;  // inner rows in 50 KB of LDS
 }
 
-hipError_t launch_experts(const ExpertArgs &a, hipStream_t stream) {
+hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
+    a.k_inverse = (uint32_t(1) << 31) / a.k + 1;
     const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
     hipError_t e;
     if (experts_by_token(a.n, a.k, a.experts, a.inner)) {
