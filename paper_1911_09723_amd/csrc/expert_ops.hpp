@@ -82,7 +82,7 @@ struct ExpertArgs {
     float *xs, *hs, *h;
     void *z;    // f32, or f16 with scales zs [pairs][hb]
     float *zs;
-    uint32_t k_inverse;  // set by launch_experts: above 2^31 / k by at most 1
+    uint32_t k_inverse, ib_inverse;  // set by launch_experts: above 2^31 / k and 2^31 / ib by at most 1
 };
 
 // Whether a call runs token by token, each pair reading its expert's weights, instead of

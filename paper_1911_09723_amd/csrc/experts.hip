@@ -19,6 +19,11 @@ __device__ __forceinline__ int32_t token_of(const ExpertArgs &a, int32_t pair) {
     return static_cast<int32_t>(static_cast<uint64_t>(pair) * a.k_inverse >> 31);
 }
 
+// block / ib, for the at most 384 blocks of a token's inner rows and those up to 32 past them.
+__device__ __forceinline__ int32_t choice_of(const ExpertArgs &a, int32_t block) {
+    return static_cast<int32_t>(static_cast<uint64_t>(block) * a.ib_inverse >> 31);
+}
+
 // Pairs (token, choice) sorted by expert: workgroup e finds the places of expert
 // e's pairs.  It counts, over all pairs, those of lower experts (its first place)
 // and its own, then hands out its places in the order of the pairs; no workgroup
@@ -405,7 +410,7 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
     if (c0 >= a.inner)
         return;
     const int32_t pitch = a.hb * kBlock;
-    const T *x = static_cast<const T *>(a.x) + (pair / a.k) * a.ldx;
+    const T *x = static_cast<const T *>(a.x) + token_of(a, pair) * a.ldx;
     constexpr int U = 2;
     float v[U][16];
     auto load_x = [&](int32_t k0) {
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
     };
     load_x(lane * 16);  // asked for before the id, which the weights' addresses wait for
     const int32_t id = a.ids[pair];
-    const bool some = id >= 0 && id < a.experts;  // else any expert's weights, and no result
+    const bool some = id >= 0 && id < a.experts;  // else any expert's weights, and zeros
     const int64_t e = some ? id : 0;
     const uint8_t *row[2 * kTokenChannels];
 #pragma unroll
@@ -466,8 +471,8 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
 #pragma unroll
     for (int i = 0; i < kTokenChannels; ++i) {
         const float h = gated<true>(sum_lanes(acc[i]), sum_lanes(acc[i + kTokenChannels]));
-        if (lane == 0 && some && c0 + i < a.inner)
-            a.h[static_cast<int64_t>(pair) * a.inner + c0 + i] = h;
+        if (lane == 0 && c0 + i < a.inner)
+            a.h[static_cast<int64_t>(pair) * a.inner + c0 + i] = some ? h : 0.0f;
     }
 }
 
@@ -478,42 +483,48 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t token = blockIdx.y, ch = min(static_cast<int32_t>(blockIdx.x) * 8 + wave, a.hidden - 1);
-    const int32_t pitch = a.ib * kBlock, chunks = (pitch + 1023) / 1024, items = a.k * chunks;
+    const int32_t pitch = a.ib * kBlock;
     const int32_t *ids = a.ids + token * a.k;
     const float *weights = a.weights + token * a.k;
     float *scales = reinterpret_cast<float *>(lds + a.k * pitch);
     constexpr int U = 8;
     u4 w[U];
     float s[U];
-    // item: choice item / chunks, channels 1024 (item % chunks) + 16 lane; without a term: times 0
-    auto load = [&](int32_t first) {
+    // items: choices, in each 1024 channels at a time, 16 a lane; without a term: times 0
+    struct Item {
+        int32_t j, k0;
+    };
+    auto step = [&](Item &i) {
+        i.k0 += 1024;
+        if (i.k0 >= pitch)
+            i = {i.j + 1, 0};
+    };
+    auto load = [&](Item i) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t item = min(first + u, items - 1), j = item / chunks, k = (item - j * chunks) * 1024 + lane * 16;
+            const int32_t j = min(i.j, a.k - 1), k = i.k0 + lane * 16;
             const int32_t e = ids[j], at = min(k, pitch - 16);
-            const bool there = first + u < items && k < pitch && e >= 0 && e < a.experts;
+            const bool there = i.j < a.k && k < pitch && e >= 0 && e < a.experts;
             const int64_t of = e >= 0 && e < a.experts ? e : 0;
             w[u] = stream16(a.w2 + (of * a.hidden + ch) * pitch + at);
             s[u] = there ? a.s2[(of * a.hb + ch / kBlock) * a.ib + at / kBlock] * weights[j] : 0.0f;
+            step(i);
         }
     };
     // inner rows to codes, 8 values a thread; the first are asked for before the ids, which
-    // the weights' addresses wait for.  Rows of ids that are no expert's were not written: zeros.
+    // the weights' addresses wait for
     const int l = threadIdx.x & 15, groups = 512 / 16, blocks = a.k * a.ib;
     float v[8];
     auto load_h = [&](int32_t i) {
-        const int32_t j = i / a.ib, c = (i - j * a.ib) * kBlock + 8 * l;
+        const int32_t j = choice_of(a, i), c = (i - j * a.ib) * kBlock + 8 * l;
         load8_tail(a.h + (static_cast<int64_t>(token) * a.k + j) * a.inner + c, i < blocks ? a.inner - c : 0,
                    a.inner % 4 == 0, v);
     };
     load_h(threadIdx.x >> 4);
-    load(0);
+    Item item{0, 0};
+    load(item);
     for (int32_t i = threadIdx.x >> 4; i < blocks; i += groups) {
-        const int32_t j = i / a.ib, c = (i - j * a.ib) * kBlock + 8 * l;
-        const bool there = static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(a.experts);
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-            v[n] = there ? v[n] : 0.0f;
+        const int32_t j = choice_of(a, i), c = (i - j * a.ib) * kBlock + 8 * l;
         uint32_t m = most8(v);
 #pragma unroll
         for (int d = 1; d < 16; d *= 2)
@@ -526,13 +537,13 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
     }
     __syncthreads();
     float acc = 0.0f;
-    for (int32_t first = 0; first < items; first += U) {
-        if (first > 0)
-            load(first);
+    while (item.j < a.k) {
+        if (item.j + item.k0 > 0)
+            load(item);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t item = min(first + u, items - 1), j = item / chunks;
-            const int32_t at = min((item - j * chunks) * 1024 + lane * 16, pitch - 16);
+            const int32_t j = min(item.j, a.k - 1), at = min(item.k0 + lane * 16, pitch - 16);
+            step(item);
             float v[16];
             code_values(*reinterpret_cast<const u4 *>(lds + j * pitch + at), v);
             const float d = dot16(v, w[u]) * (scales[j * a.ib + at / kBlock] * s[u]);
@@ -671,6 +682,7 @@ bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner) {
 
 hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
     a.k_inverse = (uint32_t(1) << 31) / a.k + 1;
+    a.ib_inverse = (uint32_t(1) << 31) / a.ib + 1;
     const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
     hipError_t e;
     if (experts_by_token(a.n, a.k, a.experts, a.inner)) {
