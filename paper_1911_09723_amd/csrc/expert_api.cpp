@@ -83,11 +83,18 @@ spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t
     return SPCONV_OK;
 }
 
-// Rows that the product's kernel does not quantise itself go through the workspace: codes, then scales.
-int64_t linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
-    if (x_dtype == SPCONV_FP8 || n == 0 || cout == 0 || spconv::linear_takes_rows(n, cin, cout))
-        return 0;
-    return code_bytes(n, cin) + align16(static_cast<int64_t>(n) * blocks_of(cin) * 4);
+// A call's workspace: rows that the product's kernel does not quantise itself, as codes and
+// scales, then the sums of workgroups that share the input channels.
+struct LinearSpace {
+    int64_t rows, sums;
+};
+LinearSpace linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
+    if (n == 0 || cout == 0)
+        return {0, 0};
+    const bool as_is = x_dtype == SPCONV_FP8 || spconv::linear_takes_rows(n, cin, cout);
+    const int64_t splits = spconv::linear_splits(n, cin, cout), cells = static_cast<int64_t>(n) * ((cout + 3) / 4 * 4);
+    return {as_is ? 0 : code_bytes(n, cin) + align16(static_cast<int64_t>(n) * blocks_of(cin) * 4),
+            splits > 1 ? splits * cells * 4 : 0};
 }
 
 constexpr int32_t kMostExpertChannels = 32768;
@@ -183,8 +190,10 @@ spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32_t n, int32
         return set_error(SPCONV_E_ARG, "bytes is NULL");
     *bytes = 0;
     const spconv_status st = check_linear(x_dtype, n, cin, cout);
-    if (st == SPCONV_OK)
-        *bytes = linear_workspace(x_dtype, n, cin, cout);
+    if (st == SPCONV_OK) {
+        const LinearSpace space = linear_workspace(x_dtype, n, cin, cout);
+        *bytes = space.rows + space.sums;
+    }
     return st;
 }
 
@@ -214,7 +223,8 @@ spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx
     if (!aligned(x, codes ? 16 : size_of(x_dtype)) || !aligned(w, 16) || !aligned(y, size_of(y_dtype)) ||
         !aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(workspace, 16))
         return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size, codes and the workspace to 16 bytes");
-    const int64_t kb = blocks_of(cin), need = linear_workspace(x_dtype, n, cin, cout);
+    const LinearSpace space = linear_workspace(x_dtype, n, cin, cout);
+    const int64_t kb = blocks_of(cin), need = space.rows + space.sums;
     if (need > 0 && (!workspace || workspace_bytes < need))
         return set_error(SPCONV_E_ARG, "the workspace is smaller than spconv_linear_fp8_workspace says");
     const Range in[] = {{x, codes ? code_bytes(n, cin) : span(n, cin, ldx, size_of(x_dtype))},
@@ -241,7 +251,8 @@ spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, int64_t ldx
     a.cout = cout;
     a.kb = static_cast<int32_t>(kb);
     clamp_of(act, a.lo, a.hi);
-    if (need > 0) {
+    a.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + space.rows);
+    if (space.rows > 0) {
         uint8_t *q = static_cast<uint8_t *>(workspace);
         float *scale = reinterpret_cast<float *>(q + code_bytes(n, cin));
         const hipError_t e = spconv::launch_quantize_rows(x, x_dtype, ldx, n, cin, q, scale, s);

@@ -30,6 +30,7 @@ struct LinearArgs {
     const float *ws;     // [ceil(cout / 128)][kb]
     const float *bias;   // [cout] or null
     void *y;
+    float *partial;      // [splits][n][cout rounded up to 4] where workgroups share the input channels
     int32_t x_type, y_type;
     int32_t n, cin, cout, kb;
     float lo, hi;
@@ -37,6 +38,8 @@ struct LinearArgs {
 
 // Whether rows that are not quantised yet are quantised inside the product's kernel.
 bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout);
+// How many workgroups share the input channels of a tile; above 1 the call needs `partial`.
+int32_t linear_splits(int32_t n, int32_t cin, int32_t cout);
 hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream);
 
 // Router: ids and weights [n][k] from logits [n][experts] (row stride ld elements).

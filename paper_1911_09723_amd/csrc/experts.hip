@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
-    tile_product<S, EXACT, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, lds, wave, lane);
+    tile_product<S, EXACT, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, a.hb, lds, wave, lane);
 
     const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(S::kThreads) down_tile(ExpertArgs a, int32_t c
     const float *ws = a.s2 + (static_cast<int64_t>(tile.expert) * a.hb + min(cw, a.hidden - 1) / kBlock) * a.ib;
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
-    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.ib, lds, wave, lane);
+    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.ib, a.ib, lds, wave, lane);
     const int32_t ch = cw + (lane >> 4) * 4;
     float inverse[S::NT];
     if constexpr (HALF) {

@@ -29,10 +29,15 @@ __device__ __forceinline__ void finish(const LinearArgs &a, bool wide, int32_t r
     store4(a.y, a.y_type, static_cast<int64_t>(row) * a.cout + ch, v, a.cout - ch, wide);
 }
 
-template <class S, bool EXACT>
-__global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t ctiles, int32_t ttiles, bool wide) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// PARTS: groups of wavefronts that share the blocks of the input channels, each
+// its own run of them in its own buffers; the first adds up the sums.  SPLIT:
+// workgroups share them, too (gridDim.y), and linear_join adds up theirs.
+template <class S, bool EXACT, int PARTS, bool SPLIT>
+__global__ void __launch_bounds__(PARTS *S::kThreads) linear_tile(LinearArgs a, int32_t ctiles, int32_t ttiles, bool wide) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char all_lds[];
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = PARTS > 1 ? all / S::kWaves : 0, wave = all - part * S::kWaves;
+    unsigned char *lds = all_lds + part * S::kLds;
     // neighbouring tiles on one XCD, in groups of 8 row tiles: they share W and X in its L2
     const int32_t per = gridDim.x / kXcds, id = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
     if (id >= ctiles * ttiles)
@@ -41,11 +46,14 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
     const int32_t ct = in / high, tt = group * 8 + in - ct * high;
     const int32_t c0 = ct * S::BC, t0 = tt * S::BT;
     const uint32_t pitch = a.kb * kBlock;
+    const int32_t run = SPLIT ? blockIdx.y * PARTS + part : part, runs = SPLIT ? gridDim.y * PARTS : PARTS;
+    const int32_t loops = (a.kb + runs - 1) / runs, b0 = min(run * loops, a.kb - 1);
+    const int32_t kb = min(max(a.kb - run * loops, 0), loops);
     TileSource<S> from;
-    from.w = a.w + static_cast<int64_t>(c0) * pitch;
-    from.x = static_cast<const uint8_t *>(a.x) + static_cast<int64_t>(t0) * pitch;
-    from.w_bytes = min(S::BC, a.cout - c0) * pitch;
-    from.x_bytes = min(S::BT, a.n - t0) * pitch;
+    from.w = a.w + static_cast<int64_t>(c0) * pitch + b0 * kBlock;
+    from.x = static_cast<const uint8_t *>(a.x) + static_cast<int64_t>(t0) * pitch + b0 * kBlock;
+    from.w_bytes = min(S::BC, a.cout - c0) * pitch - b0 * kBlock;
+    from.x_bytes = min(S::BT, a.n - t0) * pitch - b0 * kBlock;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const int line = tile_line<S>(wave, lane, i);
@@ -55,17 +63,46 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
             from.at[i] = line - S::BC < a.n - t0 ? (line - S::BC) * pitch + tile_byte(line, lane) : from.x_bytes;
     }
     from.rows = a.n - t0;
-    from.xs = a.xs;
+    from.xs = a.xs + static_cast<int64_t>(b0) * a.n;
     from.xs_at = min(t0 + wave % (S::BT / 64) * 64 + lane, a.n - 1) * 4u;
     from.xs_step = a.n * 4u;
-    from.xs_bytes = from.xs_step * a.kb;
+    from.xs_bytes = from.xs_step * (a.kb - b0);
     const int wc = channel_part<S>(wave);
     const int32_t cw = c0 + wc * S::NC * 16;
-    const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb;
+    const float *ws = a.ws + static_cast<int64_t>(min(cw, a.cout - 1) / kBlock) * a.kb + b0;
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
-    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, a.kb, lds, wave, lane);
+    tile_product<S, EXACT, false>(acc, total, from, ws, nullptr, kb, loops, lds, wave, lane);
+    if constexpr (PARTS > 1) {
+        constexpr int kPieces = S::NC * S::NT;
+        static_assert(kPieces * S::kThreads * 16 <= S::kLds, "a part's sums fit where its operands were");
+        auto at = [&](int p, int c, int t) {
+            return reinterpret_cast<f4 *>(all_lds + p * S::kLds) + (wave * kPieces + c * S::NT + t) * 64 + lane;
+        };
+        if (part > 0)
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+                for (int t = 0; t < S::NT; ++t)
+                    *at(part, c, t) = acc[c][t];
+        __syncthreads();
+        if (part > 0)
+            return;
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p)
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+                for (int t = 0; t < S::NT; ++t)
+                    acc[c][t] += *at(p, c, t);
+    }
     const int32_t ch = cw + (lane >> 4) * 4;
+    if constexpr (SPLIT) {
+        const int32_t pitch4 = (a.cout + 3) / 4 * 4;
+        store_tile<S>(acc, a.partial + static_cast<int64_t>(blockIdx.y) * a.n * pitch4, kF32, t0, a.n - t0, ch, pitch4, true,
+                      wave, lane, lds, [](f4 v, int, int) { return v; });
+        return;
+    }
     f4 bias[S::NC];
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
@@ -79,6 +116,20 @@ __global__ void __launch_bounds__(S::kThreads) linear_tile(LinearArgs a, int32_t
                 v[i] = clamp_to(v[i], a.lo, a.hi);
         return v;
     });
+}
+
+// The sum of `splits` workgroups' results, in their order; a thread has four channels.
+__global__ void __launch_bounds__(256) linear_join(LinearArgs a, int32_t splits, bool wide) {
+    const int32_t pieces = (a.cout + 3) / 4;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int32_t row = static_cast<int32_t>(id / pieces), ch = static_cast<int32_t>(id - row * static_cast<int64_t>(pieces)) * 4;
+    if (row >= a.n)
+        return;
+    const f4 *from = reinterpret_cast<const f4 *>(a.partial) + id;
+    f4 sum = *from;
+    for (int32_t s = 1; s < splits; ++s)
+        sum += from[static_cast<int64_t>(s) * a.n * pieces];
+    finish(a, wide, row, ch, sum);
 }
 
 // XT: Fp8 (codes) or the type of rows that are quantised here.
@@ -166,15 +217,15 @@ hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_
     return hipGetLastError();
 }
 
-template <class S, bool EXACT>
-hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream) {
+template <class S, bool EXACT, int PARTS = 1, bool SPLIT = false>
+hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream, int32_t splits = 1) {
     const int64_t ct = (a.cout + S::BC - 1) / S::BC, tt = (a.n + S::BT - 1) / S::BT;
-    static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void *>(linear_tile<S, EXACT>),
-                                                        hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void *>(linear_tile<S, EXACT, PARTS, SPLIT>),
+                                                        hipFuncAttributeMaxDynamicSharedMemorySize, PARTS * S::kLds);
     if (ready != hipSuccess)
         return ready;
     const int64_t grid = (ct * tt + kXcds - 1) / kXcds * kXcds;
-    linear_tile<S, EXACT><<<static_cast<uint32_t>(grid), S::kThreads, S::kLds, stream>>>(
+    linear_tile<S, EXACT, PARTS, SPLIT><<<dim3(static_cast<uint32_t>(grid), splits), PARTS * S::kThreads, PARTS * S::kLds, stream>>>(
         a, static_cast<int32_t>(ct), static_cast<int32_t>(tt), wide);
     return hipGetLastError();
 }
@@ -192,18 +243,47 @@ bool linear_takes_rows(int32_t n, int32_t cin, int32_t cout) {
     return n <= kStreamRows && (blocks_of(cin) + kStreamWaves - 1) / kStreamWaves * ((groups + 255) / 256) <= 2;
 }
 
-// Which kernel.  Up to 32 rows the stream kernel: the weight's bytes bound it (24 x 4096 ->
-// 4096: 8.7 us, the smallest tiles 11.5; 64 rows 14.5 and 11.5).  Each of its workgroups reads all
-// rows, as many bytes as of the weight at 16 rows: 32 channels a workgroup in place of 16 where
-// that still gives every compute unit one (with the rows' conversion, 32 x 8192 -> 8192: 31.4 to
-// 24.5 us, 16 x 4096 -> 8192 12.5 to 11.1; 32 x 8192 -> 4096 17.8 and 22.0).  Then tiles, the largest that
-// still give the card's 256 compute units work: a tile of 64 x 64 four blocks deep where there
-// are no more of those than compute units (128 rows of 4096 -> 4096: 11.7 us against 15.2 in
-// tiles of 128 x 64), 256 x 256 from 112 on (2048 rows: 47.8 against 52.1; 1536: 39.4 against 39.0
-// with 96), 128 x 64 between, three blocks deep while a compute unit has one (512 rows: 17.0
-// against 22.3 two deep; 1024 rows, two each: 27.7 against 25.9).  Results in 32 bits take the
-// exact products, at half the rate: 256 x 256 from 192 on (2048 rows, 128 tiles: 97 us against 69
-// in tiles of 128 x 128; 8192 rows, 512 tiles: 207 against 252).
+namespace {
+int64_t tiles_of(int32_t n, int32_t cout, int32_t channels, int32_t rows) {
+    return static_cast<int64_t>((cout + channels - 1) / channels) * ((n + rows - 1) / rows);
+}
+
+// Whether codes take the stream kernel: few rows of a small weight, whose time is that of a few
+// loads one after the other (16 x 2048 -> 4096: 4.5 us, the smallest tiles 5.9; 16 x 4096 -> 4096
+// 7.0 and 8.2).  Every workgroup of it reads all rows, so that a larger weight is read faster by
+// tiles: 16 x 5120 -> 5120 13.6 and 9.4, 1 x 8192 -> 8192 15.1 and 13.4; 24 x 2048 -> 4096 5.2 and
+// 5.8, x 8192 7.6 and 5.9.  Results in 32 bits take exact products, half as fast in tiles and as fast
+// here: 24 x 8192 -> 8192 20.7 and 25, but 32 x 2048 -> 32768 27.7 and 16.5.
+bool streams(int32_t n, int32_t kb, int32_t cout, bool exact) {
+    const int64_t weight = static_cast<int64_t>(kb) * kBlock * cout;
+    return n <= kStreamRows && (weight < (n <= 16 ? 24 << 20 : 16 << 20) || (exact && cout <= 24576));
+}
+}  // namespace
+
+// A compute unit takes in some 75 GB/s here, so a long axis of few tiles is shared by up to eight
+// workgroups a tile, at the price of a second launch that adds up their sums: 128 x 8192 -> 1024
+// 10.6 us, unshared 15.4; 32 x 16384 -> 512 9.8, over the stream kernel 24.6; 128 x 4096 -> 2048 9.7 and
+// 9.4, 128 x 8192 -> 4096 (128 tiles) 14.7 and 16.4, the launch's 3.5 us on the host not counted.
+int32_t linear_splits(int32_t n, int32_t cin, int32_t cout) {
+    const int64_t tiles = tiles_of(n, cout, 64, 64);
+    if (n <= 16 || blocks_of(cin) < 48 || tiles > 64)
+        return 1;
+    return static_cast<int32_t>(std::min<int64_t>(256 / tiles, 8));
+}
+
+// Which kernel.  Few rows of a small weight the stream kernel, with 32 channels a workgroup in
+// place of 16 where every compute unit still has one (results in 32 bits, 32 x 8192 -> 8192: 22 us,
+// with 16 channels 29; 16-bit ones of 32 x 8192 -> 4096 15.4, with 32 channels 19.6).  Then tiles, the
+// largest that still give the card's 256 compute units work.  64 x 64, four blocks deep, where there are
+// no more of those than compute units; from 8 blocks on two groups of wavefronts share them, since one
+// wavefront a SIMD waits for itself at every step of a block (128 x 4096 -> 4096 9.8 us, one group
+// 11.7; 128 x 512 -> 8192 4.6 and 4.2).  64 x 64, two on a compute unit, also where one tile has all rows and
+// there are enough to level out (64 x 4096 -> 128256 121 us, 128 x 64 146; 16 x 2048 -> 32768
+// 12.7 and 19.5; 64 x 4096 -> 20000, 313 tiles, 18.7 and 16.4).  256 x 256 from 112 on (2048 rows of
+// 4096 -> 4096: 47.8 against 52.1; 1536: 39.4 against 39.0 with 96), 128 x 64 between, three blocks
+// deep while a compute unit has one (512 rows: 17.0 against 22.3 two deep; 1024 rows, two each: 27.7
+// against 25.9).  Results in 32 bits: 256 x 256 from 192 on (2048 rows, 128 tiles: 97 us against 69 in
+// tiles of 128 x 128; 8192 rows, 512 tiles: 207 against 252).
 hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
     const bool wide_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size_of(a.x_type) % 16 == 0;
     const bool wide = a.cout % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
@@ -211,18 +291,30 @@ hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
         return a.x_type == kF32   ? stream_launch<float, 1, 1>(a, wide_x, wide, stream)
                : a.x_type == kF16 ? stream_launch<_Float16, 1, 1>(a, wide_x, wide, stream)
                                   : stream_launch<__bf16, 1, 1>(a, wide_x, wide, stream);
-    const bool pairs = a.n > 8 && a.cout >= 8192;
-    if (a.n <= 16)
-        return pairs ? stream_launch<Fp8, 1, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 1, 1>(a, wide_x, wide, stream);
-    if (a.n <= kStreamRows)
-        return pairs ? stream_launch<Fp8, 2, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 2, 1>(a, wide_x, wide, stream);
-    auto tiles = [&](int32_t channels, int32_t rows) {
-        return static_cast<int64_t>((a.cout + channels - 1) / channels) * ((a.n + rows - 1) / rows);
-    };
     const bool exact = a.y_type == kF32;
-    if (tiles(64, 64) <= 256)
-        return exact ? tile_launch<TileShape<64, 64, 1, 4, 4>, true>(a, wide, stream)
-                     : tile_launch<TileShape<64, 64, 1, 4, 4>, false>(a, wide, stream);
+    const int32_t splits = linear_splits(a.n, a.cin, a.cout);
+    if (streams(a.n, a.kb, a.cout, exact) && splits == 1) {
+        const bool pairs = a.n > 8 && a.cout >= 8192;
+        if (a.n <= 16)
+            return pairs ? stream_launch<Fp8, 1, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 1, 1>(a, wide_x, wide, stream);
+        return pairs ? stream_launch<Fp8, 2, 2>(a, wide_x, wide, stream) : stream_launch<Fp8, 2, 1>(a, wide_x, wide, stream);
+    }
+    auto tiles = [&](int32_t channels, int32_t rows) { return tiles_of(a.n, a.cout, channels, rows); };
+    if (splits > 1) {
+        const hipError_t e = exact ? tile_launch<TileShape<64, 64, 1, 4, 4>, true, 2, true>(a, wide, stream, splits)
+                                   : tile_launch<TileShape<64, 64, 1, 4, 4>, false, 2, true>(a, wide, stream, splits);
+        if (e != hipSuccess)
+            return e;
+        const int64_t pieces = static_cast<int64_t>(a.n) * ((a.cout + 3) / 4);
+        linear_join<<<static_cast<uint32_t>((pieces + 255) / 256), 256, 0, stream>>>(a, splits, wide);
+        return hipGetLastError();
+    }
+    const int64_t small = tiles(64, 64);
+    if (small <= 256 || (small > 384 && a.n <= 64))
+        return a.kb < 8 || small > 256 ? exact ? tile_launch<TileShape<64, 64, 1, 4, 4>, true>(a, wide, stream)
+                                : tile_launch<TileShape<64, 64, 1, 4, 4>, false>(a, wide, stream)
+               : exact  ? tile_launch<TileShape<64, 64, 1, 4, 4>, true, 2>(a, wide, stream)
+                        : tile_launch<TileShape<64, 64, 1, 4, 4>, false, 2>(a, wide, stream);
     if (tiles(256, 256) >= (exact ? 192 : 112))
         return exact ? tile_launch<TileShape<256, 256, 2, 4>, true>(a, wide, stream)
                      : tile_launch<TileShape<256, 256, 2, 4>, false>(a, wide, stream);

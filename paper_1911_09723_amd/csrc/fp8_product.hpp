@@ -110,10 +110,12 @@ __device__ __forceinline__ void wait_all() {
 // acc[c][t] += the products over kb blocks; ws0, ws1: the scales by block of
 // the first and of the second half (HALVES) of the wavefront's channel pieces;
 // total[t] += the scales' products, whose sum times 128 * 448^2 no result exceeds.
+// loops: kb, or more where other wavefronts of the workgroup, which it meets
+// block by block, have more blocks; those past kb are zeros.
 template <class S, bool EXACT, bool HALVES>
 __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&total)[S::NT],
                                              const TileSource<S> &from, const float *ws0, const float *ws1, int32_t kb,
-                                             unsigned char *lds, int wave, int lane) {
+                                             int32_t loops, unsigned char *lds, int wave, int lane) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources
     const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     // Every wavefront issues the same number of loads a block, so that it can
@@ -144,7 +146,7 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
     int32_t at_stage = 0, to_stage = (S::kStages - 1) * S::kStage;
     auto next_stage = [](int32_t at) { return at == (S::kStages - 1) * S::kStage ? 0 : at + S::kStage; };
     if (wt * S::NT * 16 >= from.rows) {  // no rows of its own: only its share of the loads
-        for (int32_t b = 0; b < kb; ++b) {
+        for (int32_t b = 0; b < loops; ++b) {
             wait_all<(S::kStages - 2) * kEach>();
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
@@ -159,8 +161,9 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
     auto fragment = [&](const unsigned char *p) {
         return join(*reinterpret_cast<const u4 *>(p + at), *reinterpret_cast<const u4 *>(p + (at ^ 64)));
     };
+    const int32_t last = max(kb, 1) - 1;
     float sw0 = uniform_load(ws0), sw1 = HALVES ? uniform_load(ws1) : 0.0f;
-    for (int32_t b = 0; b < kb; ++b) {
+    for (int32_t b = 0; b < loops; ++b) {
         wait_all<(S::kStages - 2) * kEach>();
         const unsigned char *buf = lds + at_stage;
         unsigned char *other = lds + to_stage;
@@ -216,8 +219,8 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
         for (int t = 0; t < S::NT; ++t)
             add(S::NC - 1, t);
         // the next block's scales: asked for here, so that no later wait for operands in LDS is one for them
-        sw0 = uniform_load(ws0 + min(b + 1, kb - 1));
-        sw1 = HALVES ? uniform_load(ws1 + min(b + 1, kb - 1)) : 0.0f;
+        sw0 = uniform_load(ws0 + min(b + 1, last));
+        sw1 = HALVES ? uniform_load(ws1 + min(b + 1, last)) : 0.0f;
     }
     __syncthreads();
 #endif

@@ -116,13 +116,28 @@ def test_linear_many_rows_or_channels(dtype, n, cin, cout):
 # few rows: quantised in the product or before it, one or two pieces of channels a workgroup
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("n,cin,cout", [(1, 2100, 8211), (9, 2100, 8211), (17, 4500, 8211), (32, 640, 8200),
-                                        (3, 8100, 70), (20, 4224, 300), (32, 900, 2050), (8, 2049, 8190)])
+                                        (3, 8100, 70), (20, 4224, 300), (32, 900, 2050), (8, 2049, 8190),
+                                        (2, 5000, 5150), (27, 4090, 4100), (5, 1030, 25000), (50, 300, 24700)])
 def test_linear_few_rows(dtype, n, cin, cout):
     note("linear %s n %d cin %d cout %d" % (dtype, n, cin, cout))
     w, b = _layer(cout, cin, 5, True)
     layer = sp.Fp8Linear.from_dense(w, b)
     x = _rows(n, cin, dtype, 6, 1)
     _check_linear(layer.run(x), x, layer, b, "none", dtype)
+
+
+# many input channels and few tiles: workgroups share a tile's input channels
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,cin,cout,act", [(33, 2048, 1, "none"), (40, 8192, 130, "relu"), (100, 4100, 66, "none"),
+                                            (65, 16400, 64, "relu6"), (300, 2300, 257, "none"), (129, 8070, 515, "none")])
+def test_linear_many_input_channels(dtype, n, cin, cout, act):
+    note("linear %s n %d cin %d cout %d" % (dtype, n, cin, cout))
+    w, b = _layer(cout, cin, 7, True)
+    layer = sp.Fp8Linear.from_dense(w, b, act)
+    x = _rows(n, cin, dtype, 8)
+    _check_linear(layer.run(x), x, layer, b, act, dtype)
+    q = sp.quantize_fp8(x)
+    _check_linear(layer.run(q[0], q[1], dtype=torch_dtype(dtype)), x, layer, b, act, dtype, q)
 
 
 @pytest.mark.parametrize("n", [1, 16, 17, 40, 64, 65, 300])
