@@ -321,6 +321,9 @@ hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
     if (tiles(128, 64) <= 256)
         return exact ? tile_launch<TileShape<128, 64, 2, 2, 3>, true>(a, wide, stream)
                      : tile_launch<TileShape<128, 64, 2, 2, 3>, false>(a, wide, stream);
+    if (tiles(128, 128) <= 256)
+        return exact ? tile_launch<TileShape<128, 128, 2, 4, 3>, true>(a, wide, stream)
+                     : tile_launch<TileShape<128, 128, 2, 4, 3>, false>(a, wide, stream);
     return exact ? tile_launch<TileShape<128, 128, 2, 2>, true>(a, wide, stream)
                  : tile_launch<TileShape<128, 64, 2, 2>, false>(a, wide, stream);
 }
