@@ -280,10 +280,12 @@ int32_t linear_splits(int32_t n, int32_t cin, int32_t cout) {
 // 11.7; 128 x 512 -> 8192 4.6 and 4.2).  64 x 64, two on a compute unit, also where one tile has all rows and
 // there are enough to level out (64 x 4096 -> 128256 121 us, 128 x 64 146; 16 x 2048 -> 32768
 // 12.7 and 19.5; 64 x 4096 -> 20000, 313 tiles, 18.7 and 16.4).  256 x 256 from 112 on (2048 rows of
-// 4096 -> 4096: 47.8 against 52.1; 1536: 39.4 against 39.0 with 96), 128 x 64 between, three blocks
-// deep while a compute unit has one (512 rows: 17.0 against 22.3 two deep; 1024 rows, two each: 27.7
-// against 25.9).  Results in 32 bits: 256 x 256 from 192 on (2048 rows, 128 tiles: 97 us against 69 in
-// tiles of 128 x 128; 8192 rows, 512 tiles: 207 against 252).
+// 4096 -> 4096: 47.8 against 52.1; 1536: 39.4 against 39.0 with 96).  Between, while a compute unit has
+// one: 128 x 64 with twice four wavefronts from 16 blocks on (300 rows of 4096 -> 4096: 12.9 us, with four
+// 15.4; 192 of 8192 -> 8192 24.1 and 28.2), with eight below (1900 rows of 1024 -> 1000: 6.8, four 7.7),
+// then 128 x 128 three deep (1024 rows of 4096 -> 4096: 23.4, 128 x 64 two deep 25.9); else 128 x 64
+// two deep (1400 rows of 512 -> 4096: 8.5 against 10.9).  Results in 32 bits: 256 x 256 from 192 on (2048 rows,
+// 128 tiles: 97 us against 69 in tiles of 128 x 128; 8192 rows, 512 tiles: 207 against 252).
 hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
     const bool wide_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size_of(a.x_type) % 16 == 0;
     const bool wide = a.cout % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
@@ -319,8 +321,10 @@ hipError_t launch_linear_fp8(const LinearArgs &a, hipStream_t stream) {
         return exact ? tile_launch<TileShape<256, 256, 2, 4>, true>(a, wide, stream)
                      : tile_launch<TileShape<256, 256, 2, 4>, false>(a, wide, stream);
     if (tiles(128, 64) <= 256)
-        return exact ? tile_launch<TileShape<128, 64, 2, 2, 3>, true>(a, wide, stream)
-                     : tile_launch<TileShape<128, 64, 2, 2, 3>, false>(a, wide, stream);
+        return a.kb < 16 ? exact ? tile_launch<TileShape<128, 64, 2, 4, 4>, true>(a, wide, stream)
+                                 : tile_launch<TileShape<128, 64, 2, 4, 4>, false>(a, wide, stream)
+               : exact   ? tile_launch<TileShape<128, 64, 2, 2, 3>, true, 2>(a, wide, stream)
+                         : tile_launch<TileShape<128, 64, 2, 2, 3>, false, 2>(a, wide, stream);
     if (tiles(128, 128) <= 256)
         return exact ? tile_launch<TileShape<128, 128, 2, 4, 3>, true>(a, wide, stream)
                      : tile_launch<TileShape<128, 128, 2, 4, 3>, false>(a, wide, stream);

@@ -104,7 +104,8 @@ def test_linear_matches_64_bits(dtype, n, cin, cout, act, bias, extra):
 # every tile shape, and grids of several thousand tiles
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("n,cin,cout", [(70, 1300, 70), (300, 640, 2100), (1030, 384, 1030), (2050, 256, 2050),
-                                        (4099, 384, 3075), (12, 128, 70000), (70000, 128, 12)])
+                                        (4099, 384, 3075), (12, 128, 70000), (70000, 128, 12), (500, 2200, 3900),
+                                        (450, 260, 4100), (790, 1100, 4000)])
 def test_linear_many_rows_or_channels(dtype, n, cin, cout):
     note("linear %s n %d cin %d cout %d" % (dtype, n, cin, cout))
     w, b = _layer(cout, cin, 3, True)
