@@ -38,9 +38,10 @@ namespace spconv {
 // its product, when the result is there.  The compiler would undo both (it
 // gathers the loads and lets each multiply-add wait for its product), hence the
 // scheduling barriers and the empty assembly that pins the sums.  8192 x 4096 ->
-// 4096 in this order: 128 us, without it 143 to 167 us; the multiply-adds cost
-// 10 us of that, and half of what is left over the products' own 70 us is the
-// start of each block, where all wavefronts read their first operands at once.
+// 4096 over tiles of 256 x 256: 117 to 125 us (2.2 to 2.35 PFLOP/s; a large library
+// product without block scales 94), in the compiler's order 143 to 167.  What bounds it
+// are the products with their operands' reads from LDS (103 us alone; the matrix units
+// work 44% of the time at 2.4 GHz), then the multiply-adds by the scales (10 us).
 // ---------------------------------------------------------------------------
 template <int BC_, int BT_, int WC_, int WT_, int STAGES_ = 2>
 struct TileShape {
@@ -253,7 +254,8 @@ __device__ __forceinline__ void store_whole(const f4 (&acc)[S::NC][S::NT], void 
 // The same for 16-bit results and rows of whole 16-byte pieces: through the
 // wavefront's own part of LDS, from where each store writes whole 128-byte
 // lines (straight from the registers it writes 32 bytes of each of 16 rows;
-// 134 MB of results: 133 us against 111 us in all for 32768 x 1024 -> 2048).
+// 134 MB of results: 133 us against 111 us in all for 32768 x 1024 -> 2048 among
+// other work; alone it takes 79, 13 of them for the stores).
 // Piece p of row r lies at p ^ r % pieces: rows start on the same bank.
 template <class S, int TYPE, class F>
 __device__ __forceinline__ void store_lines(const f4 (&acc)[S::NC][S::NT], void *y, int64_t row, int32_t rows, int32_t ch,
@@ -320,7 +322,9 @@ __device__ __forceinline__ void store_tile(const f4 (&acc)[S::NC][S::NT], void *
 // of the input channels dealt to the wavefronts of a workgroup in turn.
 // Nothing is shared between wavefronts but the final sum, so operands go from
 // global memory (rows: from L2) to registers in the instruction's layout.  What
-// bounds it is the weight's bytes, so the products are the exact ones.
+// bounds it is a chain of a few loads and the bytes of weight and rows, so the
+// products are the exact ones (1 x 1024 -> 1024: 3.1 us, 1 x 4096 -> 4096: 6.2 us,
+// 2.7 TB/s).
 // ---------------------------------------------------------------------------
 
 // A lane's part (32 of 128 channels) of one row and block, and the block's scale.

@@ -1,7 +1,9 @@
 // Matrices to 8-bit floating point with a scale for each block (fp8.hpp).
 //
 // One pass over the data: a block stays in registers between the search for
-// its largest magnitude and the conversion.
+// its largest magnitude and the conversion.  What bounds it is traffic (8192 x
+// 4096 bf16, 101 MB: 23.8 us, 4.3 TB/s; a large copy 4.76), below some MB the
+// launch (16 x 1280: 2.8 us).
 #include <algorithm>
 
 #include "expert_ops.hpp"

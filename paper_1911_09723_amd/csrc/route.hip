@@ -71,10 +71,11 @@ __device__ __forceinline__ void sort_keys(uint64_t (&key)[PER], int32_t (&id)[PE
 // A wavefront a token; a lane holds PER neighbouring experts, so that the
 // lowest lane of a tie holds the lowest expert.  What bounds it is the count of
 // instructions (16384 x 256 logits, 16.8 MB, 8 groups of 32, k = 8: 23 us
-// against 3.5 for the bytes): a 64-bit exponential for each logit, then for each
-// choice a maximum over the lanes.  Each lane sorts its keys once, so that a
-// choice looks at one key a lane, compares the upper 32 bits first, and only the
-// winner's lane moves its next key up.
+// against 3.7 for the bytes; 714 a wavefront, 19 us at the rate of issue): a
+// 64-bit exponential for each logit, then for each choice a maximum over the
+// lanes.  Each lane sorts its keys once, so that a choice looks at one key a
+// lane, compares the upper 32 bits first, and only the winner's lane moves its
+// next key up.
 // lds: a wavefront's scores, and its keys where groups do not fall on whole lanes.
 template <typename T, int PER>
 __global__ void __launch_bounds__(256) route_kernel(RouteArgs a, bool wide) {
