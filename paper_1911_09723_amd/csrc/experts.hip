@@ -626,11 +626,6 @@ hipError_t launch_combine(const ExpertArgs &a, bool wide, hipStream_t stream) {
                                : combine_by<T, 1>(a, wide, stream);
 }
 
-template <typename F>
-hipError_t allow_lds(F *kernel, int bytes) {
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 // Most tiles of `high` rows that pairs of so many experts can make.
 int64_t most_tiles(const ExpertArgs &a, int32_t high) {
     return std::min<int64_t>(a.pairs, a.pairs / high + std::min(a.experts, a.pairs));
@@ -642,7 +637,8 @@ uint32_t tile_grid(int64_t tiles, int64_t columns) {
 
 template <class S, bool EXACT>
 hipError_t gated_tiles(const ExpertArgs &a, hipStream_t stream) {
-    static const hipError_t ready = allow_lds(gated_tile<S, EXACT>, S::kLds);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t ready = allow_lds(gated_tile<S, EXACT>, S::kLds, done);
     if (ready != hipSuccess)
         return ready;
     gated_tile<S, EXACT><<<tile_grid(most_tiles(a, S::BT), a.ib), S::kThreads, S::kLds, stream>>>(a, a.ib);
@@ -651,7 +647,8 @@ hipError_t gated_tiles(const ExpertArgs &a, hipStream_t stream) {
 
 template <class S, bool EXACT, bool HALF>
 hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
-    static const hipError_t ready = allow_lds(down_tile<S, EXACT, HALF>, S::kLds);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t ready = allow_lds(down_tile<S, EXACT, HALF>, S::kLds, done);
     if (ready != hipSuccess)
         return ready;
     const int32_t columns = (a.hidden + S::BC - 1) / S::BC;

@@ -220,8 +220,8 @@ hipError_t stream_launch(const LinearArgs &a, bool wide_x, bool wide, hipStream_
 template <class S, bool EXACT, int PARTS = 1, bool SPLIT = false>
 hipError_t tile_launch(const LinearArgs &a, bool wide, hipStream_t stream, int32_t splits = 1) {
     const int64_t ct = (a.cout + S::BC - 1) / S::BC, tt = (a.n + S::BT - 1) / S::BT;
-    static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void *>(linear_tile<S, EXACT, PARTS, SPLIT>),
-                                                        hipFuncAttributeMaxDynamicSharedMemorySize, PARTS * S::kLds);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t ready = allow_lds(linear_tile<S, EXACT, PARTS, SPLIT>, PARTS * S::kLds, done);
     if (ready != hipSuccess)
         return ready;
     const int64_t grid = (ct * tt + kXcds - 1) / kXcds * kXcds;

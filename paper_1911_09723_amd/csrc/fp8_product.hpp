@@ -11,9 +11,27 @@
 // lane then holds one row of X (one scale) and four neighbouring channels.
 #pragma once
 
+#include <atomic>
+
 #include "fp8.hpp"
 
 namespace spconv {
+
+// Allows a kernel its LDS, once on each device (done: one bit for each).
+template <typename F>
+hipError_t allow_lds(F *kernel, int bytes, std::atomic<uint64_t> &done) {
+    int device = 0;
+    if (const hipError_t e = hipGetDevice(&device); e != hipSuccess)
+        return e;
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (done.load() & bit)
+        return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess)
+        done.fetch_or(bit);
+    return e;
+}
 
 // ---------------------------------------------------------------------------
 // Tile core.  BC channels x BT rows, WC x WT wavefronts, each NC x NT pieces of
