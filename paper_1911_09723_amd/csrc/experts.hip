@@ -656,6 +656,20 @@ hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// A tile's rows by the rows that an expert has on average, as long as compute units, which hold
+// one tile of any size (LDS; so the smaller ones are three blocks deep), have one.  Measured
+// (64 experts, bf16): 250 rows each 196 us, in tiles of 64 rows 251; 150 rows 151 us in tiles of
+// 128, 175 in 256 and in 64; 50 rows 111 in 64, 123 in 128.  By tiles at most: 256 rows each, second
+// products in 64 tiles of 256 rows 26.4 us, 96 of 128 rows 18.2, 160 of 64 14.2; 1024 rows each, 160 of 256
+// 30.8, 288 of 128 36.2; 128 rows each, 128 tiles of 128 18.9, 192 of 64 14.6, but 256 of 128 10.1, 384
+// of 64 13.2.
+int32_t tile_rows(const ExpertArgs &a, int64_t columns, bool big) {
+    const int64_t each = a.pairs / a.experts;
+    if (big && each >= 192 && most_tiles(a, 256) * columns >= 144)
+        return 256;
+    return each >= 96 && most_tiles(a, 128) * columns >= 144 ? 128 : 64;
+}
+
 template <typename T>
 hipError_t prepare(const ExpertArgs &a, hipStream_t stream) {
     const bool wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
@@ -704,37 +718,34 @@ hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
     e = a.type == kF32 ? prepare<float>(a, stream) : a.type == kF16 ? prepare<_Float16>(a, stream) : prepare<__bf16>(a, stream);
     if (e != hipSuccess)
         return e;
-    // The tile's rows by the rows an expert has on average; a compute unit holds one tile of
-    // any of these (LDS), so the smaller ones are three blocks deep.  Measured (64 experts,
-    // bf16): 250 rows each 196 us, in tiles of 64 rows 251; 150 rows 151 us in tiles of 128, 175
-    // in 256 and in 64; 50 rows 111 in 64, 123 in 128.
     using Small = TileShape<256, 64, 2, 4, 3>;
     using Mid = TileShape<256, 128, 2, 4, 3>;
     using Big = TileShape<256, 256, 2, 4>;
-    const int64_t each = a.pairs / a.experts;
     // The inner rows are rounded to codes again, which turns an error of 4e-5 into one of
     // 1.5e-3: below the rounding of bf16 results, not of others, whose first products are exact.
     // The results' error is their own: exact products for 32 bits only.
-    if (a.type == kBf16)
-        e = each >= 192  ? gated_tiles<Big, false>(a, stream)
-            : each >= 96 ? gated_tiles<Mid, false>(a, stream)
-                         : gated_tiles<Small, false>(a, stream);
+    const bool exact = a.type != kBf16;
+    const int32_t first = tile_rows(a, a.ib, !exact), second = tile_rows(a, (a.hidden + 255) / 256, true);
+    if (exact)
+        e = first == 128 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
     else
-        e = each >= 96 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
+        e = first == 256   ? gated_tiles<Big, false>(a, stream)
+            : first == 128 ? gated_tiles<Mid, false>(a, stream)
+                           : gated_tiles<Small, false>(a, stream);
     if (e != hipSuccess)
         return e;
     if (a.type == kF32)
-        e = each >= 192  ? down_tiles<Big, true, false>(a, stream)
-            : each >= 96 ? down_tiles<Mid, true, false>(a, stream)
-                         : down_tiles<Small, true, false>(a, stream);
+        e = second == 256   ? down_tiles<Big, true, false>(a, stream)
+            : second == 128 ? down_tiles<Mid, true, false>(a, stream)
+                            : down_tiles<Small, true, false>(a, stream);
     else if (a.type == kF16)
-        e = each >= 192  ? down_tiles<Big, false, false>(a, stream)
-            : each >= 96 ? down_tiles<Mid, false, false>(a, stream)
-                         : down_tiles<Small, false, false>(a, stream);
+        e = second == 256   ? down_tiles<Big, false, false>(a, stream)
+            : second == 128 ? down_tiles<Mid, false, false>(a, stream)
+                            : down_tiles<Small, false, false>(a, stream);
     else
-        e = each >= 192  ? down_tiles<Big, false, true>(a, stream)
-            : each >= 96 ? down_tiles<Mid, false, true>(a, stream)
-                         : down_tiles<Small, false, true>(a, stream);
+        e = second == 256   ? down_tiles<Big, false, true>(a, stream)
+            : second == 128 ? down_tiles<Mid, false, true>(a, stream)
+                            : down_tiles<Small, false, true>(a, stream);
     if (e != hipSuccess)
         return e;
     return a.type == kBf16 ? launch_combine<_Float16>(a, wide, stream) : launch_combine<float>(a, wide, stream);

@@ -137,6 +137,19 @@ def test_experts_match_64_bits(dtype, n, experts, k, hidden, inner, extra):
     _check_experts(layer.run(x, ids, weights), x, ids, weights, layer, dtype)
 
 
+# enough tiles for those of 256 and of 128 rows, with parts of them empty
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,experts,k,hidden,inner", [(800, 8, 2, 300, 1410), (801, 8, 2, 2820, 200),
+                                                      (800, 8, 2, 2819, 130), (560, 8, 2, 300, 1157),
+                                                      (560, 8, 2, 2304, 200)])
+def test_experts_large_tiles(dtype, n, experts, k, hidden, inner):
+    note("experts %s n %d experts %d k %d hidden %d inner %d" % (dtype, n, experts, k, hidden, inner))
+    layer = _experts(experts, hidden, inner, n + hidden)
+    x = _rows(n, hidden, dtype, inner, 0)
+    ids, weights = _chosen(n, k, experts, n)
+    _check_experts(layer.run(x, ids, weights), x, ids, weights, layer, dtype)
+
+
 @pytest.mark.parametrize("n,experts", [(2, 8), (40, 8), (200, 2)])
 def test_experts_ids_that_are_none(n, experts):
     import torch
