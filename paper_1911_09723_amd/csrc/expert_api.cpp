@@ -121,7 +121,7 @@ int64_t experts_layout(spconv::ExpertArgs &a, uint8_t *base) {
         at += (bytes + 255) / 256 * 256;  // codes on whole 128-byte lines: else a product reads two for one
     };
     const int64_t pairs = a.pairs;
-    if (spconv::experts_by_token(a.n, a.k, a.experts, a.inner)) {
+    if (spconv::experts_by_token(a.n, a.k, a.experts, a.hidden, a.inner)) {
         take(a.h, pairs * a.inner * 4);
         return at;
     }

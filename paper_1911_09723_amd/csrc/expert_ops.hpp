@@ -90,7 +90,7 @@ struct ExpertArgs {
 
 // Whether a call runs token by token, each pair reading its expert's weights, instead of
 // over tiles of the rows of one expert.
-bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner);
+bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t hidden, int32_t inner);
 hipError_t launch_experts(ExpertArgs a, hipStream_t stream);
 
 }  // namespace spconv

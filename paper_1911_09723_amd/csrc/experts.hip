@@ -693,11 +693,16 @@ hipError_t gated_tokens(const ExpertArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// One or two tokens of different experts: measured (bf16, 2048 x 1024 channels, 8 of 64
-// experts) 1 token 20.5 us, over tiles 34.1; 2 tokens 29.9 and 35.4; 4 tokens 51.3 and 43.8.
-bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t inner) {
-    const int64_t pairs = static_cast<int64_t>(n) * k;
-    return n <= 2 && pairs <= 64 && pairs <= experts && k * blocks_of(inner) <= 384;  // inner rows in 50 KB of LDS
+// Token by token where pairs are of different experts mostly: one or two tokens, and a few more
+// while the weights are small, so that two launches in place of four count.  Measured (bf16, over tiles in
+// brackets): 2048 x 1024, 8 of 64 experts, 1 token 20.5 us (34.1), 2 29.9 (35.4), 4 51.3 (43.8);
+// 1024 x 512, 4 of 128, 4 tokens 17.9 (21.1), 6 22.7 (22.2); 512 x 256, 8 of 64, 4 tokens 17.6 (19.1),
+// 6 21.9 (19.1); 512 x 512, 1 of 32, 8 tokens 13.6 (17.6), 16 20.7 (17.5).
+bool experts_by_token(int32_t n, int32_t k, int32_t experts, int32_t hidden, int32_t inner) {
+    const int64_t pairs = static_cast<int64_t>(n) * k, weights = pairs * 3 * hidden * inner;
+    if (pairs > experts || k * blocks_of(inner) > 384)  // inner rows in 50 KB of LDS
+        return false;
+    return n <= 2 ? pairs <= 64 : n <= 8 && pairs <= 32 && weights <= 32 << 20;
 }
 
 hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
@@ -705,7 +710,7 @@ hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
     a.ib_inverse = (uint32_t(1) << 31) / a.ib + 1;
     const bool wide = a.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
     hipError_t e;
-    if (experts_by_token(a.n, a.k, a.experts, a.inner)) {
+    if (experts_by_token(a.n, a.k, a.experts, a.hidden, a.inner)) {
         e = a.type == kF32   ? gated_tokens<float>(a, stream)
             : a.type == kF16 ? gated_tokens<_Float16>(a, stream)
                              : gated_tokens<__bf16>(a, stream);

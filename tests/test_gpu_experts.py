@@ -137,6 +137,20 @@ def test_experts_match_64_bits(dtype, n, experts, k, hidden, inner, extra):
     _check_experts(layer.run(x, ids, weights), x, ids, weights, layer, dtype)
 
 
+# few tokens of small experts, on both sides of where they are taken one by one
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,experts,k,hidden,inner", [(3, 16, 4, 300, 200), (8, 32, 4, 1000, 130), (8, 9, 1, 257, 1030),
+                                                      (9, 32, 2, 300, 200), (8, 31, 4, 300, 200), (5, 64, 6, 1300, 900)])
+def test_experts_few_tokens(dtype, n, experts, k, hidden, inner):
+    note("experts %s n %d experts %d k %d hidden %d inner %d" % (dtype, n, experts, k, hidden, inner))
+    layer = _experts(experts, hidden, inner, n + hidden)
+    x = _rows(n, hidden, dtype, inner, 0)
+    ids, weights = _chosen(n, k, experts, n)
+    ids[n - 1, 0] = -1
+    ids[0, k - 1] = ids[1, k - 1]
+    _check_experts(layer.run(x, ids, weights), x, ids, weights, layer, dtype)
+
+
 # enough tiles for those of 256 and of 128 rows, with parts of them empty
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("n,experts,k,hidden,inner", [(800, 8, 2, 300, 1410), (801, 8, 2, 2820, 200),
