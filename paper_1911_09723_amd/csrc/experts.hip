@@ -498,7 +498,9 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
     constexpr int U = 8;
     u4 w[U];
     float s[U];
-    // items: choices, in each 1024 channels at a time, 16 a lane; without a term: times 0
+    bool on[U];
+    // items: choices, in each 1024 channels at a time, 16 a lane; those without a term (on) are
+    // left out of the sum, not multiplied by 0: what they repeat may be NaN, and a weight of 0 has one
     struct Item {
         int32_t j, k0;
     };
@@ -512,10 +514,10 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
         for (int u = 0; u < U; ++u) {
             const int32_t j = min(i.j, a.k - 1), k = i.k0 + lane * 16;
             const int32_t e = ids[j], at = min(k, pitch - 16);
-            const bool there = i.j < a.k && k < pitch && e >= 0 && e < a.experts;
+            on[u] = i.j < a.k && k < pitch && e >= 0 && e < a.experts;
             const int64_t of = e >= 0 && e < a.experts ? e : 0;
             w[u] = stream16(a.w2 + (of * a.hidden + ch) * pitch + at);
-            s[u] = there ? a.s2[(of * a.hb + ch / kBlock) * a.ib + at / kBlock] * weights[j] : 0.0f;
+            s[u] = on[u] ? a.s2[(of * a.hb + ch / kBlock) * a.ib + at / kBlock] * weights[j] : 0.0f;
             step(i);
         }
     };
@@ -555,7 +557,7 @@ __global__ void __launch_bounds__(512) down_token(ExpertArgs a) {
             float v[16];
             code_values(*reinterpret_cast<const u4 *>(lds + j * pitch + at), v);
             const float d = dot16(v, w[u]) * (scales[j * a.ib + at / kBlock] * s[u]);
-            acc += s[u] != 0.0f ? d : 0.0f;
+            acc += on[u] ? d : 0.0f;
         }
     }
     acc = sum_lanes(acc);
