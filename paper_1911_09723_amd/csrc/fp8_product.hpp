@@ -128,7 +128,7 @@ __device__ __forceinline__ void wait_all() {
 
 // acc[c][t] += the products over kb blocks; ws0, ws1: the scales by block of
 // the first and of the second half (HALVES) of the wavefront's channel pieces;
-// total[t] += the scales' products, whose sum times 128 * 448^2 no result exceeds.
+// total[t] += the scales' products without their signs, whose sum times 128 * 448^2 no result exceeds.
 // loops: kb, or more where other wavefronts of the workgroup, which it meets
 // block by block, have more blocks; those past kb are zeros.
 template <class S, bool EXACT, bool HALVES>
@@ -220,7 +220,7 @@ __device__ __forceinline__ void tile_product(f4 (&acc)[S::NC][S::NT], float (&to
                 if (c == 0) {
                     s1[t] = HALVES ? s0[t] * sw1 : 0.0f;
                     s0[t] *= sw0;
-                    total[t] += s0[t];
+                    total[t] += fabsf(s0[t]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 const int id = c * S::NT + t;

@@ -1,0 +1,96 @@
+"""How far experts' outputs may be from 64 bits, by the type of rows and results.
+
+The products' forms follow the type: f32 sums exact products in 32 bits
+throughout; f16 does so up to the inner rows, and takes the 8-bit instruction
+for the second products; bf16 takes it for both, and keeps the second products'
+results in f16 (with a power of two for each 128) before the weighted sum.
+(Token by token all sums are 32-bit ones.)
+
+Of one element (``bound``): the 8-bit instruction's cut (fp8_util.cut_bound)
+where it is used, else 2^-23 of the terms a step; f16 in between 2^-11 of a
+value, and 2^-25 of the power of two below f16's normal numbers, a power that
+is at most 2^-14 of 448^2 * 128 times the sum of the |scales' products|.
+
+Of all together (``NORM``), for well spread inputs: an error d of an inner
+value whose codes are s apart changes its code with probability d / s, and
+then by s, so the mean square of the change is d s; s is at most 2^-3 of the
+value, which makes sqrt(0.1 d) of a relative error d.  32-bit sums: d = 2^-21
+is generous, 2.2e-4; twice that for a count of changes that is small.  8-bit
+products: d = 5e-5, 2.2e-3.  The second products add 5e-5 where they are 8-bit
+ones, f16 in between 2^-11 / sqrt(3), the result's rounding as much of its unit.
+"""
+
+import numpy as np
+
+from fp8_util import (BLOCK, ROUND, SMALLEST, TOP, block_values, blocks, code_values, cut_bound, quantize_interval,
+                      quantize_ref, row_values)
+
+ROOT3 = 3.0 ** 0.5
+NORM = {"f32": 5e-4,
+        "f16": 5e-4 + 5e-5 + ROUND["f16"] / ROOT3,
+        "bf16": 2.2e-3 + 5e-5 + 2.0 ** -11 / ROOT3 + ROUND["bf16"] / ROOT3}
+
+
+def bound(x, ids, weights, layer, dtype):
+    """(y, tolerance of each element) in 64 bits."""
+    n, k = ids.shape
+    hb, ib = blocks(layer.hidden), blocks(layer.inner)
+    xq, xs = quantize_ref(x, 1)
+    xv = row_values(xq, xs, layer.hidden)
+    y, tol = np.zeros((n, layer.hidden)), np.zeros((n, layer.hidden))
+    w13, s13 = code_values(layer.w13), layer.w13_scale.cpu().numpy()
+    w2, s2 = code_values(layer.w2), layer.w2_scale.cpu().numpy()
+    for e in range(layer.experts):
+        token, slot = np.nonzero(ids == e)
+        if len(token) == 0:
+            continue
+        xe = xv[token]
+        first = []
+        for i in (0, 1):
+            w = block_values(w13[e, i], s13[e, i], layer.hidden)
+            d = np.abs(xe) @ np.abs(w).T * (BLOCK + hb + 8) * 2.0 ** -23
+            first.append((xe @ w.T, d + (cut_bound(xe, w) if dtype == "bf16" else 0)))
+        (g, dg), (u, du) = first
+        with np.errstate(over="ignore"):
+            silu = g / (1 + np.exp(-g))
+        dh = 1.1 * dg * (np.abs(u) + du) + np.abs(silu) * du + np.abs(silu * u) * 2.0 ** -20
+        hv, dv = quantize_interval(silu * u, dh)
+        w = block_values(w2[e], s2[e], layer.inner)
+        z, reach = hv @ w.T, (np.abs(hv) + dv) @ np.abs(w).T
+        dz = dv @ np.abs(w).T + reach * (BLOCK + ib + 8) * 2.0 ** -23
+        if dtype != "f32":
+            dz = dz + cut_bound(np.abs(hv) + dv, w)
+        if dtype == "bf16":
+            scales = np.maximum(np.abs(silu * u).reshape(len(token), -1), 0)
+            most = np.stack([scales[:, b:b + BLOCK].max(axis=1) for b in range(0, layer.inner, BLOCK)], axis=1)
+            total = (np.maximum(most * 1.01, 2.0 ** -100) / TOP) @ np.abs(s2[e].astype(np.float64)).T
+            total = np.repeat(total, BLOCK, axis=1)[:, :layer.hidden]
+            dz = dz + np.abs(z) * 2.0 ** -11 + total * TOP * TOP * BLOCK * 2.0 ** -39
+        p = weights[token, slot].astype(np.float64)[:, None]
+        np.add.at(y, token, z * p)
+        np.add.at(tol, token, (dz + np.abs(z) * (k + 4) * 2.0 ** -23) * np.abs(p))
+    return y, tol + np.abs(y) * ROUND[dtype] + SMALLEST[dtype]
+
+
+def reference(x, ids, weights, layer):
+    """y alone, for larger cases."""
+    xq, xs = quantize_ref(x, 1)
+    xv = row_values(xq, xs, layer.hidden)
+    y = np.zeros((ids.shape[0], layer.hidden))
+    w13, s13 = code_values(layer.w13), layer.w13_scale.cpu().numpy()
+    w2, s2 = code_values(layer.w2), layer.w2_scale.cpu().numpy()
+    for e in range(layer.experts):
+        token, slot = np.nonzero(ids == e)
+        if len(token) == 0:
+            continue
+        g, u = (xv[token] @ block_values(w13[e, i], s13[e, i], layer.hidden).T for i in (0, 1))
+        with np.errstate(over="ignore"):
+            h = (g / (1 + np.exp(-g)) * u).astype(np.float32)
+        q, s = quantize_ref(h, 1)
+        z = row_values(q, s, layer.inner) @ block_values(w2[e], s2[e], layer.inner).T
+        np.add.at(y, token, z * weights[token, slot].astype(np.float64)[:, None])
+    return y
+
+
+def norm_error(y, ref):
+    return float(np.linalg.norm(y.double().cpu().numpy() - ref) / np.linalg.norm(ref))
