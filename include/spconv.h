@@ -313,9 +313,20 @@ SPCONV_API spconv_status spconv_quantize_fp8(const void *x, spconv_dtype dtype, 
 /*
  * Dense layer with an 8-bit weight:
  *   y[t][r] = act( bias[r] + sum_c value(x[t][c]) * value(w[r][c]) )
- * The codes' products over each block of 128 input channels are summed on the
- * matrix cores in fp32 and scaled in fp32; the sum over blocks, the bias and
- * the activation are fp32, rounded once to y's type.
+ * Products of codes are exact.  Over each block of 128 input channels they are
+ * summed
+ *   in fp32 where y is F32, and where few rows (n <= 32) of a small weight take
+ *     a kernel without tiles;
+ *   else on the 8-bit matrix instruction: of each 8 neighbouring channels (0 to
+ *     7, 8 to 15, ...) it cuts every product off, toward zero, at 2^-13 of the
+ *     largest power of two among their products (codes below 2^-6 count as
+ *     2^-6), and adds the sums of 8 in fp32.  The sum of 8 is so up to 2^-10 of
+ *     their largest product off.  Over well spread values that is 4e-5 of a
+ *     block's sum (rms), below the rounding of an F16 or BF16 y; where large
+ *     products cancel each other it can be more, and the same row's result can
+ *     differ by it between calls of another n.
+ * The blocks' scales, the sum over blocks, the bias and the activation are
+ * fp32, rounded once to y's type.
  *   x           device, n rows of cin channels: x_dtype F32, F16 or BF16 with a
  *               row stride of ldx >= cin elements, quantised here as by
  *               spconv_quantize_fp8 with block_rows = 1; or FP8 codes (ldx unused)
@@ -387,8 +398,14 @@ SPCONV_API spconv_status spconv_route(const void *logits, spconv_dtype dtype, in
  *   y[t] = sum_j weights[t][j] * W2[e] q( silu(W1[e] q(x[t])) * (W3[e] q(x[t])) ),  e = ids[t][j],
  * with silu(v) = v / (1 + exp(-v)) and q the quantisation of a row as by
  * spconv_quantize_fp8 with block_rows = 1.  An id outside [0, experts) has no
- * term; a token with none gets zeros.  Products and sums are as for
- * spconv_linear_fp8; the gate is applied in fp32, y is rounded once.
+ * term; a token with none gets zeros.  A few tokens that are taken one by one
+ * (one or two; some more of small experts) sum products of codes in fp32.  Else
+ * the products with W1 and W3 are summed in fp32 for F32 and F16, those with W2
+ * for F32, and the others on the 8-bit matrix instruction with the loss that
+ * spconv_linear_fp8 describes.  The gate, scales and sums over blocks and over
+ * experts are fp32; for BF16 the products with W2 are held in fp16 until the sum
+ * over experts, with a power of two for each 128 of a row (2^-11 of a value).  y
+ * is rounded once.
  *   x        device, [n][hidden] of dtype (F32, F16 or BF16), row stride ldx >= hidden elements
  *   ids, weights  device, [n][k], as spconv_route gives them (any order)
  *   w13, w13_scale  W1 and W3 of each expert, [experts][2][inner][hidden] in

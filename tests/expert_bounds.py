@@ -6,9 +6,9 @@ for the second products; bf16 takes it for both, and keeps the second products'
 results in f16 (with a power of two for each 128) before the weighted sum.
 (Token by token all sums are 32-bit ones.)
 
-Of one element (``bound``): the 8-bit instruction's cut (fp8_util.cut_bound)
-where it is used, else 2^-23 of the terms a step; f16 in between 2^-11 of a
-value, and 2^-25 of the power of two below f16's normal numbers, a power that
+Of one element (``bound``): the 8-bit instruction's cut (fp8_cut.cut8, with
+inner rows' codes at most one step of their exponent off) where it is used, and
+2^-23 of the terms a step; f16 in between 2^-11 of a value, and 2^-25 of the power of two below f16's normal numbers, a power that
 is at most 2^-14 of 448^2 * 128 times the sum of the |scales' products|.
 
 Of all together (``NORM``), for well spread inputs: an error d of an inner
@@ -22,8 +22,9 @@ ones, f16 in between 2^-11 / sqrt(3), the result's rounding as much of its unit.
 
 import numpy as np
 
-from fp8_util import (BLOCK, ROUND, SMALLEST, TOP, block_values, blocks, code_values, cut_bound, quantize_interval,
-                      quantize_ref, row_values)
+from fp8_cut import cut8
+from fp8_util import (BLOCK, ROUND, SMALLEST, TOP, block_values, blocks, code_values, quantize_interval, quantize_ref,
+                      row_values)
 
 ROOT3 = 3.0 ** 0.5
 NORM = {"f32": 5e-4,
@@ -49,7 +50,9 @@ def bound(x, ids, weights, layer, dtype):
         for i in (0, 1):
             w = block_values(w13[e, i], s13[e, i], layer.hidden)
             d = np.abs(xe) @ np.abs(w).T * (BLOCK + hb + 8) * 2.0 ** -23
-            first.append((xe @ w.T, d + (cut_bound(xe, w) if dtype == "bf16" else 0)))
+            if dtype == "bf16":
+                d = d + cut8(xq[token], xs[:, token], w13[e, i], s13[e, i])
+            first.append((xe @ w.T, d))
         (g, dg), (u, du) = first
         with np.errstate(over="ignore"):
             silu = g / (1 + np.exp(-g))
@@ -58,12 +61,15 @@ def bound(x, ids, weights, layer, dtype):
         w = block_values(w2[e], s2[e], layer.inner)
         z, reach = hv @ w.T, (np.abs(hv) + dv) @ np.abs(w).T
         dz = dv @ np.abs(w).T + reach * (BLOCK + ib + 8) * 2.0 ** -23
+        size = np.abs(silu * u) + dh
+        most = np.maximum(np.stack([size[:, b:b + BLOCK].max(axis=1) for b in range(0, layer.inner, BLOCK)], axis=1),
+                          2.0 ** -100) * 1.01
         if dtype != "f32":
-            dz = dz + cut_bound(np.abs(hv) + dv, w)
+            codes = np.zeros((len(token), ib * BLOCK))
+            codes[:, :layer.inner] = hv / np.repeat(most / TOP, BLOCK, axis=1)[:, :layer.inner]
+            dz = dz + 2 * cut8(codes, (most / TOP).T, w2[e], s2[e])
         if dtype == "bf16":
-            scales = np.maximum(np.abs(silu * u).reshape(len(token), -1), 0)
-            most = np.stack([scales[:, b:b + BLOCK].max(axis=1) for b in range(0, layer.inner, BLOCK)], axis=1)
-            total = (np.maximum(most * 1.01, 2.0 ** -100) / TOP) @ np.abs(s2[e].astype(np.float64)).T
+            total = (most / TOP) @ np.abs(s2[e].astype(np.float64)).T
             total = np.repeat(total, BLOCK, axis=1)[:, :layer.hidden]
             dz = dz + np.abs(z) * 2.0 ** -11 + total * TOP * TOP * BLOCK * 2.0 ** -39
         p = weights[token, slot].astype(np.float64)[:, None]
