@@ -305,8 +305,8 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
 // or (HALF) in f16 with a scale for each 128 channels of a row.  The results are
 // written once and read once by the weighted sum: at 4096 tokens of 8 experts
 // and 2048 channels 537 MB in 32 bits, more than the products' operands.  An
-// f16 value is 2^-12 off at most, an eighth of the rounding of a bf16 result to
-// come.  The scale is the power of two that brings the most that the row's and
+// f16 value is 2^-11 off at most, an eighth of the rounding (2^-8) of a bf16
+// result to come.  The scale is the power of two that brings the most that the row's and
 // the weight's scales allow just below 2^15, so nothing overflows, and as the
 // sum of random codes stays some 2^10 below that most, what is lost to f16's
 // small numbers is 2^-30 of a usual value.  32768 pairs, 1024 -> 2048: 104 us, 1.32

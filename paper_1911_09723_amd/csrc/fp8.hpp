@@ -6,7 +6,7 @@
 // a tail of channels in its products.  A block's scale is a / 448 with
 // a = max(max |v|, 2^-100) over the block, a code is v * (448 / a) rounded to
 // the nearest e4m3 value, ties to even; each of these steps is one correctly
-// rounded 32-bit operation.  |v * (448 / a)| stays below 448 (1 + 2^-22), which
+// rounded 32-bit operation.  |v * (448 / a)| stays below 448 (1 + 2^-23), which
 // rounds to 448, so the conversion needs no clamp.  The floor on a keeps both
 // quotients finite and normal for blocks of zeros or of subnormal values.  An
 // infinity or a NaN makes its block's scale infinite or NaN: every product
