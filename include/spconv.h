@@ -400,9 +400,9 @@ SPCONV_API spconv_status spconv_route(const void *logits, spconv_dtype dtype, in
  * spconv_quantize_fp8 with block_rows = 1.  An id outside [0, experts) has no
  * term; a token with none gets zeros.  A few tokens that are taken one by one
  * (one or two; some more of small experts) sum products of codes in fp32.  Else
- * the products with W1 and W3 are summed in fp32 for F32 and F16, those with W2
- * for F32, and the others on the 8-bit matrix instruction with the loss that
- * spconv_linear_fp8 describes.  The gate, scales and sums over blocks and over
+ * the products with W1 and W3 are summed in fp32, those with W2 in fp32 for F32
+ * and on the 8-bit matrix instruction, with the loss that spconv_linear_fp8
+ * describes, for F16 and BF16.  The gate, scales and sums over blocks and over
  * experts are fp32; for BF16 the products with W2 are held in fp16 until the sum
  * over experts, with a power of two for each 128 of a row (2^-11 of a value).  y
  * is rounded once.

@@ -132,13 +132,9 @@ __global__ void __launch_bounds__(1024) prepare_rows(ExpertArgs a, int32_t row_g
                          wide);
 }
 
-// g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each.
-// EXACT: g log2(e) is taken to twice 32 bits so that the exponential stays
-// there; else it is up to |g| last places off, far less than 8-bit products are.
-template <bool EXACT>
+// g / (1 + exp(-g)) * u.  exp2 and the reciprocal are one last place off each;
+// g log2(e) is taken to twice 32 bits so that the exponential stays there.
 __device__ __forceinline__ float gated(float g, float u) {
-    if constexpr (!EXACT)
-        return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;
     const float t = g * -1.44269504f, rest = fmaf(g, -1.44269504f, -t) + g * -1.92596299e-8f;
     const float e = __builtin_amdgcn_exp2f(t);
     const float exact = fabsf(t) < 128.0f ? fmaf(e, rest * 0.693147181f, e) : e;  // else 0 or infinite
@@ -211,11 +207,11 @@ __device__ __forceinline__ bool find_tile(const int32_t *offsets, int32_t expert
 // wavefront holds 64 gate and the same 64 up channels, so that the gate is
 // applied in its registers; the block's largest magnitude is joined over the
 // two wavefronts that share its rows.  32768 pairs of 64 experts, 2048 -> 2 x
-// 1024: 177 us, 1.55 PFLOP/s; with exactly 512 rows an expert 161 to 168.  Bound by
-// the products and the weights' way in (470 MB read, 2.9 TB/s), then the gate
-// itself (13 us of VALU).  200 pairs of 32 experts, 1280 -> 2 x 960 exact: 17 us,
-// the weights at 4.6 TB/s.
-template <class S, bool EXACT>
+// 1024: 326 us, 0.84 PFLOP/s.  Bound by issue: the conversions of codes and the
+// gate take the vector units 48% of the time, the products, at half the 8-bit
+// rate, the matrix units 34%; 634 MB read, 2.05 TB/s.  200 pairs of 32 experts,
+// 1280 -> 2 x 960: 17 us, the weights at 4.6 TB/s.
+template <class S>
 __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t columns) {
     static_assert(S::BC == 256 && S::WC == 2, "a wavefront holds half a block of gate and of up channels");
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -251,7 +247,7 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
     from.xs_bytes = from.xs_step * a.hb;
     f4 acc[S::NC][S::NT] = {};
     float total[S::NT] = {};
-    tile_product<S, EXACT, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, a.hb, lds, wave, lane);
+    tile_product<S, true, true>(acc, total, from, ws, ws + static_cast<int64_t>(a.ib) * a.hb, a.hb, a.hb, lds, wave, lane);
 
     const int wc = channel_part<S>(wave), wt = row_part<S>(wave);
     float *most = reinterpret_cast<float *>(lds + S::BT * kBlock);  // [2][BT]
@@ -266,7 +262,7 @@ __global__ void __launch_bounds__(S::kThreads) gated_tile(ExpertArgs a, int32_t 
             for (int c = 0; c < HC; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float h = gated<EXACT>(acc[c][t][i], acc[c + HC][t][i]);  // channels past the last: 0
+                    const float h = gated(acc[c][t][i], acc[c + HC][t][i]);  // channels past the last: 0
                     acc[c][t][i] = h;
                     m[t] = max(m[t], magnitude(h));
                 }
@@ -478,7 +474,7 @@ __global__ void __launch_bounds__(256) gated_token(ExpertArgs a, bool wide) {
     }
 #pragma unroll
     for (int i = 0; i < kTokenChannels; ++i) {
-        const float h = gated<true>(sum_lanes(acc[i]), sum_lanes(acc[i + kTokenChannels]));
+        const float h = gated(sum_lanes(acc[i]), sum_lanes(acc[i + kTokenChannels]));
         if (lane == 0 && c0 + i < a.inner)
             a.h[static_cast<int64_t>(pair) * a.inner + c0 + i] = some ? h : 0.0f;
     }
@@ -637,13 +633,13 @@ uint32_t tile_grid(int64_t tiles, int64_t columns) {
     return static_cast<uint32_t>((tiles * columns + kXcds - 1) / kXcds * kXcds);
 }
 
-template <class S, bool EXACT>
+template <class S>
 hipError_t gated_tiles(const ExpertArgs &a, hipStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    const hipError_t ready = allow_lds(gated_tile<S, EXACT>, S::kLds, done);
+    const hipError_t ready = allow_lds(gated_tile<S>, S::kLds, done);
     if (ready != hipSuccess)
         return ready;
-    gated_tile<S, EXACT><<<tile_grid(most_tiles(a, S::BT), a.ib), S::kThreads, S::kLds, stream>>>(a, a.ib);
+    gated_tile<S><<<tile_grid(most_tiles(a, S::BT), a.ib), S::kThreads, S::kLds, stream>>>(a, a.ib);
     return hipGetLastError();
 }
 
@@ -660,8 +656,9 @@ hipError_t down_tiles(const ExpertArgs &a, hipStream_t stream) {
 
 // A tile's rows by the rows that an expert has on average, as long as compute units, which hold
 // one tile of any size (LDS; so the smaller ones are three blocks deep), have one.  Measured
-// (64 experts, bf16): 250 rows each 196 us, in tiles of 64 rows 251; 150 rows 151 us in tiles of
-// 128, 175 in 256 and in 64; 50 rows 111 in 64, 123 in 128.  By tiles at most: 256 rows each, second
+// (calls of 64 experts of 2048 x 1024 in bf16, by the first products' tiles): 512 rows each 477 us in
+// tiles of 128, 516 in 256, 559 in 64; 150 rows 198, 262, 213; 100 rows 160, 198, 171; 50 rows 122, 169,
+// 121; so the first products' are of 128 rows at most.  By tiles at most: 256 rows each, second
 // products in 64 tiles of 256 rows 26.4 us, 96 of 128 rows 18.2, 160 of 64 14.2; 1024 rows each, 160 of 256
 // 30.8, 288 of 128 36.2; 128 rows each, 128 tiles of 128 18.9, 192 of 64 14.6, but 256 of 128 10.1, 384
 // of 64 13.2.
@@ -728,17 +725,12 @@ hipError_t launch_experts(ExpertArgs a, hipStream_t stream) {
     using Small = TileShape<256, 64, 2, 4, 3>;
     using Mid = TileShape<256, 128, 2, 4, 3>;
     using Big = TileShape<256, 256, 2, 4>;
-    // The inner rows are rounded to codes again, which turns an error of 4e-5 into one of
-    // 1.5e-3: below the rounding of bf16 results, not of others, whose first products are exact.
-    // The results' error is their own: exact products for 32 bits only.
-    const bool exact = a.type != kBf16;
-    const int32_t first = tile_rows(a, a.ib, !exact), second = tile_rows(a, (a.hidden + 255) / 256, true);
-    if (exact)
-        e = first == 128 ? gated_tiles<Mid, true>(a, stream) : gated_tiles<Small, true>(a, stream);
-    else
-        e = first == 256   ? gated_tiles<Big, false>(a, stream)
-            : first == 128 ? gated_tiles<Mid, false>(a, stream)
-                           : gated_tiles<Small, false>(a, stream);
+    // The inner rows are rounded to codes again, which would turn the 8-bit instruction's error into
+    // many times itself (4e-5 of well spread values into 1.2e-3, with loud channels into more than the
+    // rounding of a bf16 result), so the first products are exact for every type.  The results' error
+    // is their own: exact products for 32 bits only.
+    const int32_t first = tile_rows(a, a.ib, false), second = tile_rows(a, (a.hidden + 255) / 256, true);
+    e = first == 128 ? gated_tiles<Mid>(a, stream) : gated_tiles<Small>(a, stream);
     if (e != hipSuccess)
         return e;
     if (a.type == kF32)

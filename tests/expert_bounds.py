@@ -1,23 +1,24 @@
 """How far experts' outputs may be from 64 bits, by the type of rows and results.
 
-The products' forms follow the type: f32 sums exact products in 32 bits
-throughout; f16 does so up to the inner rows, and takes the 8-bit instruction
-for the second products; bf16 takes it for both, and keeps the second products'
-results in f16 (with a power of two for each 128) before the weighted sum.
-(Token by token all sums are 32-bit ones.)
+The first products are exact and summed in 32 bits for every type, since their
+results are rounded to codes again.  So are the second products for f32; f16 and
+bf16 take the 8-bit instruction for them, and bf16 keeps their results in f16
+(with a power of two for each 128) before the weighted sum.  (Token by token all
+sums are 32-bit ones.)
 
-Of one element (``bound``): the 8-bit instruction's cut (fp8_cut.cut8, with
-inner rows' codes at most one step of their exponent off) where it is used, and
-2^-23 of the terms a step; f16 in between 2^-11 of a value, and 2^-25 of the power of two below f16's normal numbers, a power that
-is at most 2^-14 of 448^2 * 128 times the sum of the |scales' products|.
+Of one element (``bound``): 2^-23 of the terms a step, for the second products'
+8-bit sums their cut (fp8_cut.cut8, with inner rows' codes at most one step of
+their exponent off); f16 in between 2^-11 of a value, and 2^-25 of the power of
+two below f16's normal numbers, a power that is at most 2^-14 of 448^2 * 128
+times the sum of the |scales' products|.
 
-Of all together (``NORM``), for well spread inputs: an error d of an inner
-value whose codes are s apart changes its code with probability d / s, and
-then by s, so the mean square of the change is d s; s is at most 2^-3 of the
-value, which makes sqrt(0.1 d) of a relative error d.  32-bit sums: d = 2^-21
-is generous, 2.2e-4; twice that for a count of changes that is small.  8-bit
-products: d = 5e-5, 2.2e-3.  The second products add 5e-5 where they are 8-bit
-ones, f16 in between 2^-11 / sqrt(3), the result's rounding as much of its unit.
+Of all together, relative, for well spread inner rows: an error d of an inner
+value whose codes are s apart changes its code with probability d / s, and then
+by s, so the mean square of the change is d s; s is at most 2^-3 of the value,
+which makes sqrt(0.1 d) of a relative error d.  32-bit sums: d = 2^-21 is
+generous, 2.2e-4; twice that for a count of changes that is small.  The second
+products add 5e-5 where they are 8-bit ones, f16 in between 2^-11 / sqrt(3):
+``BESIDES``.  The result's rounding is at most 1 / sqrt(3) of its unit: ``NORM``.
 """
 
 import numpy as np
@@ -27,9 +28,8 @@ from fp8_util import (BLOCK, ROUND, SMALLEST, TOP, block_values, blocks, code_va
                       row_values)
 
 ROOT3 = 3.0 ** 0.5
-NORM = {"f32": 5e-4,
-        "f16": 5e-4 + 5e-5 + ROUND["f16"] / ROOT3,
-        "bf16": 2.2e-3 + 5e-5 + 2.0 ** -11 / ROOT3 + ROUND["bf16"] / ROOT3}
+BESIDES = {"f32": 5e-4, "f16": 5e-4 + 5e-5, "bf16": 5e-4 + 5e-5 + 2.0 ** -11 / ROOT3}
+NORM = {t: BESIDES[t] + ROUND[t] / ROOT3 for t in BESIDES}
 
 
 def bound(x, ids, weights, layer, dtype):
@@ -49,10 +49,7 @@ def bound(x, ids, weights, layer, dtype):
         first = []
         for i in (0, 1):
             w = block_values(w13[e, i], s13[e, i], layer.hidden)
-            d = np.abs(xe) @ np.abs(w).T * (BLOCK + hb + 8) * 2.0 ** -23
-            if dtype == "bf16":
-                d = d + cut8(xq[token], xs[:, token], w13[e, i], s13[e, i])
-            first.append((xe @ w.T, d))
+            first.append((xe @ w.T, np.abs(xe) @ np.abs(w).T * (BLOCK + hb + 8) * 2.0 ** -23))
         (g, dg), (u, du) = first
         with np.errstate(over="ignore"):
             silu = g / (1 + np.exp(-g))
