@@ -55,8 +55,9 @@ typedef enum {
 typedef enum {
     SPCONV_F32 = 0,
     SPCONV_F16 = 1,
-    SPCONV_BF16 = 2, /* the operators of 8-bit products, routing and experts only */
-    SPCONV_FP8 = 3   /* 8-bit e4m3 codes with scales (below); as BF16, and only where a call says so */
+    SPCONV_BF16 = 2, /* the operators of 8-bit and 4-bit products, norms, routing, experts and sampling only */
+    SPCONV_FP8 = 3,  /* 8-bit e4m3 codes with scales (below); as BF16, and only where a call says so */
+    SPCONV_MXFP4 = 4 /* 4-bit e2m1 codes with powers of two (below); as FP8 */
 } spconv_dtype;
 
 typedef enum { SPCONV_ACT_NONE = 0, SPCONV_ACT_RELU = 1, SPCONV_ACT_RELU6 = 2 } spconv_act;
@@ -352,6 +353,154 @@ SPCONV_API spconv_status spconv_linear_fp8(const void *x, spconv_dtype x_dtype, 
  * negative size, bad dtype), SPCONV_E_SHAPE as above. */
 SPCONV_API spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout,
                                                      int64_t *bytes);
+
+/* ---------------------------------------------------------------------------
+ * Dense layers in 4-bit floating point, with a power of two for each 32
+ * channels (the OCP microscaling form MXFP4).
+ *
+ * The 4-bit form of a row-major matrix [rows][cols], rows and weights alike.
+ * With lines = ceil(cols / 256):
+ *   codes   [rows][128 * lines] bytes, two e2m1 codes a byte, the lower column in
+ *           the lower four bits (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 the
+ *           sign); zeros past cols; 16-byte aligned
+ *   scales  [lines][rows][8] bytes, byte b of a line for its columns 32 b to
+ *           32 b + 31: the exponent plus 127, 255 for NaN; 16-byte aligned
+ * An element's value is its code's value times two to its block's exponent.
+ * Calls launch on `stream` as the 8-bit layers above do.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Quantise: the exponent e of a block is the least, from -127 on, for which its
+ * largest magnitude a rounds to a code and not past the largest: a / 2^e < 7.
+ * Codes are x / 2^e rounded once to the nearest value, ties to the even code; a
+ * value that rounds to zero keeps its sign.  A block that holds an infinity or a
+ * NaN has scale 255 and codes 0, so that every product with it is NaN.
+ *   x       device, [rows][cols] of dtype (F32, F16 or BF16), row stride ldx >= cols elements
+ *   q, scale  out, in the form above
+ * rows == 0 or cols == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
+ * cols, bad dtype or alignment, overlap), SPCONV_E_SHAPE (rows * ceil(cols /
+ * 256) of 2^28 or more, cols above 2^30, ldx above 2^34), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_quantize_mxfp4(const void *x, spconv_dtype dtype, int64_t ldx, int32_t rows,
+                                               int32_t cols, void *q, void *scale, void *stream);
+
+/*
+ * Dense layer with a 4-bit weight:
+ *   y[t][r] = act( bias[r] + sum_c value(x[t][c]) * value(w[r][c]) )
+ * Products of codes and their sums over a block of 32 are exact; the powers of
+ * two, the sum over blocks, the bias and the activation are fp32, rounded once to
+ * y's type.
+ *   x           device, n rows of cin channels: x_dtype F32, F16 or BF16 with a
+ *               row stride of ldx >= cin elements, quantised here as by
+ *               spconv_quantize_mxfp4; or MXFP4 codes (ldx unused)
+ *   x_scale     the scales of MXFP4 codes; NULL for other types
+ *   w, w_scale  the weight [cout][cin] in 4-bit form
+ *   bias        device, cout floats, or NULL
+ *   y           device, [n][cout] of y_dtype (F32, F16 or BF16)
+ *   workspace   device, 16-byte aligned, of at least the size that
+ *               spconv_linear_mxfp4_workspace gives (NULL where that is 0); its
+ *               contents mean nothing before or after the call's work
+ * n == 0 or cout == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
+ * cin, bad dtype, act or alignment, x_scale missing or not asked for, workspace
+ * too small, overlap), SPCONV_E_SHAPE (cin == 0 with outputs, cin or cout above
+ * 2^22, n * ceil(cin / 256) of 2^27 or more, cout * ceil(cin / 256) of 2^28 or
+ * more, n * cout of 2^36 or more, ldx above 2^34), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_linear_mxfp4(const void *x, spconv_dtype x_dtype, int64_t ldx, const void *x_scale,
+                                             const void *w, const void *w_scale, const float *bias, spconv_act act,
+                                             void *y, spconv_dtype y_dtype, int32_t n, int32_t cin, int32_t cout,
+                                             void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace for such a call, host only.  Errors: SPCONV_E_ARG (NULL,
+ * negative size, bad dtype), SPCONV_E_SHAPE as above. */
+SPCONV_API spconv_status spconv_linear_mxfp4_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout,
+                                                       int64_t *bytes);
+
+/* ---------------------------------------------------------------------------
+ * Between a model's layers and after the last.  Calls launch on `stream` as the
+ * 8-bit layers above do.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front and
+ * 8-bit rows behind it where asked:
+ *   h     = x + residual                              (x where residual is NULL)
+ *   total = h, rounded once
+ *   v     = h / sqrt( sum h^2 / cols + eps ) * gain   (gain 1 where NULL)
+ *   y     = v, rounded once;  q, scale = v as by spconv_quantize_fp8 with block_rows = 1
+ * all in fp32: the norm is that of h before it is rounded, codes are those of v
+ * in fp32.  Squares are fp32, too: a row whose sum of squares passes 2^128 gives zeros.
+ *   x         device, [rows][cols] of dtype (F32, F16 or BF16), row stride ldx >= cols elements
+ *   residual  device, of residual_dtype with row stride ldr, or NULL
+ *   total     out, of residual_dtype with row stride ldt, or NULL
+ *   gain      device, cols values of gain_dtype, or NULL
+ *   y         out, of y_dtype with row stride ldy, or NULL
+ *   q, scale  out, codes [rows][128 kb] and scales [kb][rows], kb = ceil(cols /
+ *             128), as FP8 rows of spconv_linear_fp8; or both NULL
+ * residual_dtype, gain_dtype and y_dtype are dtype or F32; one whose pointer is
+ * NULL is not looked at.  total and y may each be exactly x or residual (the
+ * same address, row stride and element size); else outputs overlap neither
+ * inputs nor each other.  At least one of y and q is given.  Columns of strided
+ * rows past cols are neither read nor written.
+ * rows == 0 or cols == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, a stride
+ * below cols, bad dtype or alignment, eps negative, infinite or NaN, total
+ * without residual, overlap), SPCONV_E_UNSUPPORTED (a type that is neither dtype
+ * nor F32), SPCONV_E_SHAPE (rows * ceil(cols / 128) of 2^27 or more, cols above
+ * 2^30, a stride above 2^34), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_rms_norm(const void *x, spconv_dtype dtype, int64_t ldx, const void *residual,
+                                         spconv_dtype residual_dtype, int64_t ldr, void *total, int64_t ldt,
+                                         const void *gain, spconv_dtype gain_dtype, float eps, void *y,
+                                         spconv_dtype y_dtype, int64_t ldy, void *q, float *scale, int32_t rows,
+                                         int32_t cols, void *stream);
+
+/*
+ * The next token of each row of logits, from a given random number.  With l a
+ * row's logits, m their maximum, and t, k, p, least its temperature, top_k,
+ * top_p and min_p, a token weighs
+ *   w[i] = exp( (l[i] - m) / t )
+ * and tokens are ordered by l, the largest first, equal ones by index.  Kept are,
+ * one filter after the other,
+ *   the first k of that order                        (all where k is 0)
+ *   of these the shortest start of the order whose weight is at least p times theirs
+ *   of these the ones with w >= least;
+ * the token is the first, by index, at which the running sum of the kept weights
+ * exceeds u times their sum.  t = 0 takes the first of the order.  A token whose
+ * logit is -infinity or NaN is off: never taken, of no weight; +infinity counts as the
+ * largest finite float.  A row without a token that is on gets -1.
+ * Weights are 64-bit, in their sums multiples of 2^-42 of the largest: the choice
+ * does not hang on the order of additions, and is the same in every call.
+ *   logits  device, [n][vocab] of dtype (F32, F16 or BF16), row stride ld >= vocab elements
+ *   u       device, n floats in [0, 1); below 0 or NaN counts as 0, 1 and above as the
+ *           largest float below 1
+ *   temperatures, top_ks, top_ps, min_ps  device, n values, or NULL: then
+ *           temperature (>= 0), top_k (>= 0), top_p and min_p (in [0, 1]) hold for
+ *           every row.  Of the device's values a temperature that is not above 0
+ *           counts as 0, a top_k below 1 or above vocab as vocab, a top_p that is not
+ *           below 1 as 1 (below 0 as 0: one token), a min_p that is not above 0
+ *           as 0 and one above 1 as 1
+ *   ids     out, n int32_t
+ *   workspace  device, 16-byte aligned, at least what spconv_sample_workspace
+ *           gives (NULL where that is 0); its contents mean nothing before or
+ *           after the call's work
+ * n == 0 is a no-op.
+ * Errors: SPCONV_E_ARG (NULL pointer with work to do, bad dtype or alignment,
+ * negative n, vocab < 1, ld < vocab, a parameter out of its range, workspace too
+ * small, overlap), SPCONV_E_SHAPE (n of 2^20 or more, ld above 2^34),
+ * SPCONV_E_UNSUPPORTED (vocab above 2^20), SPCONV_E_HIP.
+ */
+SPCONV_API spconv_status spconv_sample(const void *logits, spconv_dtype dtype, int64_t ld, const float *u, int32_t n,
+                                       int32_t vocab, const float *temperatures, const int32_t *top_ks,
+                                       const float *top_ps, const float *min_ps, float temperature, int32_t top_k,
+                                       float top_p, float min_p, int32_t *ids, void *workspace,
+                                       int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace for such a call, host only.  Errors: SPCONV_E_ARG (NULL,
+ * bad dtype, negative n, vocab < 1), SPCONV_E_SHAPE and SPCONV_E_UNSUPPORTED as above. */
+SPCONV_API spconv_status spconv_sample_workspace(spconv_dtype dtype, int32_t n, int32_t vocab, int64_t *bytes);
 
 /* ---------------------------------------------------------------------------
  * Mixtures of experts: sparsity that is chosen for each token at run time.  A

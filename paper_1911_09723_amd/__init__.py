@@ -6,7 +6,8 @@ ones), and hand-written gfx950 HIP kernels compute act(W X + b) on NCHW fp32
 or fp16 tensors, optionally with a depthwise 3x3 stage fused in front.  Beside them
 stand the operators of a language model's expert layers (``experts.py``): dense
 products in 8 bits with a scale for each block of 128, a router and the chosen
-experts' networks.  This package is the thin Python binding plus the in-tree build script.
+experts' networks; and what a served model has around them (``serving.py``): norms
+that write 8-bit rows, dense products in 4 bits, and sampling.  This package is the thin Python binding plus the in-tree build script.
 """
 
 from .spconv import (  # noqa: F401
@@ -27,6 +28,8 @@ from .spconv import (  # noqa: F401
     spconv_linear,
     spconv_linear_fp8,
     spconv_linear_fp8_workspace,
+    spconv_linear_mxfp4,
+    spconv_linear_mxfp4_workspace,
     spconv_options_init,
     spconv_plan_create,
     spconv_plan_create_blocked,
@@ -45,8 +48,19 @@ from .spconv import (  # noqa: F401
     spconv_plan_set_wait_limit,
     SPCONV_FLAG_WAIT_GAVE_UP,
     spconv_quantize_fp8,
+    spconv_quantize_mxfp4,
+    spconv_rms_norm,
     spconv_route,
     spconv_run,
+    spconv_sample,
+    spconv_sample_workspace,
+)
+from .serving import (  # noqa: F401
+    Mxfp4Linear,
+    quantize_mxfp4,
+    rms_norm,
+    rms_norm_fp8,
+    sample,
 )
 from .experts import (  # noqa: F401
     ExpertLayer,

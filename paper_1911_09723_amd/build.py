@@ -23,6 +23,7 @@ LIB = os.path.join(PKG, "libspconv.so")
 
 SOURCES = ["planner.cpp", "spconv_api.cpp", "spmm_kernels.hip", "spmm_indexed.hip", "spmm_outer.hip", "spmm_half.hip", "spmm_rows.hip",
            "fp8_quantize.hip", "fp8_linear.hip", "route.hip", "experts.hip", "expert_api.cpp",
+           "norm.hip", "mxfp4_quantize.hip", "mxfp4_linear.hip", "sample.hip", "serve_api.cpp",
            "net_kernels.hip"]
 ARCH = "gfx950"
 

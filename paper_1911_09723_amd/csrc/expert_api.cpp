@@ -5,64 +5,32 @@
 
 #include <hip/hip_runtime_api.h>
 
-#include <limits>
 #include <type_traits>
 
+#include "checks.hpp"
 #include "expert_ops.hpp"
-#include "status.hpp"
 
 namespace {
 
+using spconv::align16;
+using spconv::aligned;
 using spconv::blocks_of;
+using spconv::clamp_of;
+using spconv::is_float;
+using spconv::kMostStride;
+using spconv::launched;
+using spconv::outputs_overlap;
+using spconv::Range;
 using spconv::set_error;
+using spconv::size_of;
+using spconv::span;
 
 constexpr int64_t kMostBlocks = int64_t(1) << 27;  // row blocks of a matrix: launches stay below 2^32 threads
 constexpr int64_t kMostOutputs = int64_t(1) << 36;
 constexpr int32_t kMostChannels = 1 << 22;          // a tile of 256 rows lies within 32-bit offsets
 constexpr int64_t kMostExpertBlocks = int64_t(1) << 25;  // rows by token and by pair lie within 32-bit offsets
 
-bool is_float(int32_t type) { return type == SPCONV_F32 || type == SPCONV_F16 || type == SPCONV_BF16; }
-int64_t size_of(int32_t type) { return type == SPCONV_F32 ? 4 : type == SPCONV_FP8 ? 1 : 2; }
-bool aligned(const void *p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(to) == 0; }
-
-struct Range {
-    const void *p;
-    int64_t bytes;
-};
-
-bool overlap(Range a, Range b) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-    return a.p && b.p && a.bytes > 0 && b.bytes > 0 && a0 < b0 + static_cast<uintptr_t>(b.bytes) &&
-           b0 < a0 + static_cast<uintptr_t>(a.bytes);
-}
-
-// Whether an output overlaps an input or another output.
-template <int OUT, int IN>
-bool outputs_overlap(const Range (&out)[OUT], const Range (&in)[IN]) {
-    for (int i = 0; i < OUT; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (overlap(out[i], out[j]))
-                return true;
-        for (int j = 0; j < IN; ++j)
-            if (overlap(out[i], in[j]))
-                return true;
-    }
-    return false;
-}
-
-// Bytes that strided rows span; the caller keeps the product in range.
-int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t size) { return rows ? ((rows - 1) * ld + cols) * size : 0; }
-constexpr int64_t kMostStride = int64_t(1) << 34;
-
 int64_t code_bytes(int64_t rows, int64_t cols) { return rows * blocks_of(cols) * 128; }
-int64_t align16(int64_t v) { return (v + 15) / 16 * 16; }
-
-void clamp_of(spconv_act act, float &lo, float &hi) {
-    lo = act == SPCONV_ACT_NONE ? -std::numeric_limits<float>::infinity() : 0.0f;
-    hi = act == SPCONV_ACT_RELU6 ? 6.0f : std::numeric_limits<float>::infinity();
-}
-
-spconv_status launched(hipError_t e) { return e == hipSuccess ? SPCONV_OK : spconv::set_hip_error("kernel launch", e); }
 
 // Sizes of a linear layer; SPCONV_OK also where there is nothing to do.
 spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {

@@ -1,0 +1,235 @@
+// Root-mean-square norm of rows, with the residual's addition in front and
+// 8-bit codes behind it where asked:
+//
+//     h = x + r,  total = h rounded to r's type,  y = h * (1 / sqrt(sum h^2 / cols + eps)) * gain,
+//
+// all in 32 bits; y is rounded once to its type, or quantised by blocks of 128
+// channels as quantize_fp8's rows are (fp8.hpp).  The norm is that of the
+// 32-bit h, not of the rounded total: one rounding less between x and y.
+//
+// One pass: a row stays in registers between its sum of squares and its
+// results, 8 neighbouring values a thread and piece, so that 16 lanes hold a
+// block of 128.
+#include <type_traits>
+
+#include "fp8.hpp"
+#include "serve_ops.hpp"
+
+namespace spconv {
+namespace {
+
+constexpr int kXcds = 8;
+
+struct None {};
+
+// `left` (any number) of 8 values to a row of T, rounded once.
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int left, bool wide, const float *v) {
+    if (wide && left >= 8) {
+        struct __attribute__((aligned(16))) Eight {
+            T v[8];
+        } e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            e.v[i] = static_cast<T>(v[i]);
+        *reinterpret_cast<Eight *>(p) = e;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left)
+            p[i] = static_cast<T>(v[i]);
+}
+
+// Eight values of h from column c on.
+template <typename T, typename R>
+__device__ __forceinline__ void load_sum(const NormArgs &a, int32_t row, int32_t c, float *h) {
+    load8_tail(static_cast<const T *>(a.x) + row * a.ldx + c, a.cols - c, a.wide_x, h);
+    if constexpr (!std::is_same_v<R, None>) {
+        float r[8];
+        load8_tail(static_cast<const R *>(a.residual) + row * a.ldr + c, a.cols - c, a.wide_r, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            h[i] += r[i];
+    }
+}
+
+template <typename W>
+__device__ __forceinline__ void load_gain(const NormArgs &a, int32_t c, float *g) {
+    if (a.gain) {
+        load8_tail(static_cast<const W *>(a.gain) + c, a.cols - c, a.wide_g, g);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        g[i] = 1.0f;
+}
+
+// What leaves for the eight values from column c on; every lane of a block's 16 comes here.
+template <typename T, typename R>
+__device__ __forceinline__ void finish8(const NormArgs &a, int32_t row, int32_t c, const float *h, const float *g,
+                                        float inverse) {
+    if constexpr (!std::is_same_v<R, None>)
+        if (a.total)
+            store8(static_cast<R *>(a.total) + row * a.ldt + c, a.cols - c, a.wide_t, h);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = c + i < a.cols ? h[i] * inverse * g[i] : 0.0f;
+    if (a.y) {
+        if (a.y32)
+            store8(static_cast<float *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, v);
+        else
+            store8(static_cast<T *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, v);
+    }
+    if (a.q) {
+        uint32_t m = most8(v);
+#pragma unroll
+        for (int s = 1; s < 16; s *= 2)
+            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), s)));
+        const int32_t b = c / kBlock;
+        if (b >= a.kb)
+            return;
+        const Scale s = scale_of(m);
+        *reinterpret_cast<u2 *>(a.q + static_cast<int64_t>(row) * a.kb * kBlock + c) =
+            u2{codes4(v, s.inv), codes4(v + 4, s.inv)};
+        if (c % kBlock == 0)
+            a.scale[static_cast<int64_t>(b) * a.rows + row] = s.scale;
+    }
+}
+
+// The sum over a row's THREADS threads, in a fixed order.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float *part) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2)
+        v += __shfl_xor(v, s);
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0)
+            part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = part[threadIdx.x & (THREADS / 64 - 1)];
+#pragma unroll
+        for (int s = 1; s < THREADS / 64; s *= 2)
+            v += __shfl_xor(v, s);
+    }
+    return v;
+}
+
+// The row of this thread: neighbouring rows on one XCD, so that their scales,
+// which lie side by side, leave its L2 as whole lines.
+template <int ROWS>
+__device__ __forceinline__ int32_t own_row(int threads) {
+    const int32_t per = gridDim.x / kXcds, group = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    return group * ROWS + threadIdx.x / threads;
+}
+
+// THREADS a row, VECS pieces of 8 values each.
+template <typename T, typename R, typename W, int VECS, int THREADS>
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormArgs a) {
+    __shared__ float part[16];
+    const int32_t row = own_row<THREADS < 256 ? 256 / THREADS : 1>(THREADS);
+    if (row >= a.rows)
+        return;
+    const int32_t c0 = threadIdx.x % THREADS * 8;
+    float h[VECS][8];
+#pragma unroll
+    for (int u = 0; u < VECS; ++u)
+        load_sum<T, R>(a, row, c0 + u * THREADS * 8, h[u]);
+    float sum = 0;
+#pragma unroll
+    for (int u = 0; u < VECS; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sum = fmaf(h[u][i], h[u][i], sum);
+    const float inverse = 1.0f / sqrtf(row_sum<THREADS>(sum, part) / static_cast<float>(a.cols) + a.eps);
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+        float g[8];
+        load_gain<W>(a, c0 + u * THREADS * 8, g);
+        finish8<T, R>(a, row, c0 + u * THREADS * 8, h[u], g, inverse);
+    }
+}
+
+// Rows that registers do not hold: read twice.  A thread reads what it writes
+// before it writes it, so total and y may lie where residual and x do.
+template <typename T, typename R, typename W>
+__global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
+    __shared__ float part[16];
+    const int32_t row = own_row<1>(1024);
+    if (row >= a.rows)
+        return;
+    float sum = 0;
+    for (int32_t c = threadIdx.x * 8; c < a.cols; c += 8192) {
+        float h[8];
+        load_sum<T, R>(a, row, c, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sum = fmaf(h[i], h[i], sum);
+    }
+    const float inverse = 1.0f / sqrtf(row_sum<1024>(sum, part) / static_cast<float>(a.cols) + a.eps);
+    for (int32_t c0 = 0; c0 < a.cols; c0 += 8192) {  // whole wavefronts: blocks are found across lanes
+        const int32_t c = c0 + threadIdx.x * 8;
+        float h[8], g[8];
+        load_sum<T, R>(a, row, c, h);
+        load_gain<W>(a, c, g);
+        finish8<T, R>(a, row, c, h, g, inverse);
+    }
+}
+
+template <typename T, typename R, typename W>
+hipError_t launch(const NormArgs &a, hipStream_t stream) {
+    const int32_t pieces = (a.cols + 7) / 8;
+    auto grid = [&](int rows) { return ((a.rows + rows - 1) / rows + kXcds - 1) / kXcds * kXcds; };
+    if (pieces <= 64)
+        norm_rows<T, R, W, 1, 64><<<grid(4), 256, 0, stream>>>(a);
+    else if (pieces <= 256)
+        norm_rows<T, R, W, 1, 256><<<grid(1), 256, 0, stream>>>(a);
+    else if (pieces <= 512)
+        norm_rows<T, R, W, 2, 256><<<grid(1), 256, 0, stream>>>(a);
+    else if (pieces <= 1024)
+        norm_rows<T, R, W, 4, 256><<<grid(1), 256, 0, stream>>>(a);
+    else if (pieces <= 4096)
+        norm_rows<T, R, W, 4, 1024><<<grid(1), 1024, 0, stream>>>(a);
+    else
+        norm_long<T, R, W><<<grid(1), 1024, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, typename R>
+hipError_t with_gain(const NormArgs &a, bool gain32, hipStream_t stream) {
+    if constexpr (!std::is_same_v<T, float>)
+        if (!gain32)
+            return launch<T, R, T>(a, stream);
+    return launch<T, R, float>(a, stream);
+}
+
+template <typename T>
+hipError_t with_residual(const NormArgs &a, bool residual32, bool gain32, hipStream_t stream) {
+    if (!a.residual)
+        return with_gain<T, None>(a, gain32, stream);
+    if constexpr (!std::is_same_v<T, float>)
+        if (!residual32)
+            return with_gain<T, T>(a, gain32, stream);
+    return with_gain<T, float>(a, gain32, stream);
+}
+
+bool wide(const void *p, int64_t ld, int64_t size) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
+}
+
+}  // namespace
+
+hipError_t launch_norm(NormArgs a, int32_t type, bool residual32, bool gain32, hipStream_t stream) {
+    const int64_t size = type == kF32 ? 4 : 2, of_r = residual32 ? 4 : size;
+    a.wide_x = wide(a.x, a.ldx, size);
+    a.wide_r = wide(a.residual, a.ldr, of_r);
+    a.wide_t = wide(a.total, a.ldt, of_r);
+    a.wide_g = wide(a.gain, 0, 1);
+    a.wide_y = wide(a.y, a.ldy, a.y32 ? 4 : size);
+    return type == kF32   ? with_residual<float>(a, residual32, gain32, stream)
+           : type == kF16 ? with_residual<_Float16>(a, residual32, gain32, stream)
+                          : with_residual<__bf16>(a, residual32, gain32, stream);
+}
+
+}  // namespace spconv

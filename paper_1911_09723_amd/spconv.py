@@ -20,12 +20,12 @@ LIBRARY_PATH = os.path.join(_HERE, "libspconv.so")
 OK, E_ARG, E_FORMAT, E_SHAPE, E_UNSUPPORTED, E_NOMEM, E_HIP = range(7)
 STATUS_NAMES = {0: "SPCONV_OK", 1: "SPCONV_E_ARG", 2: "SPCONV_E_FORMAT", 3: "SPCONV_E_SHAPE",
                 4: "SPCONV_E_UNSUPPORTED", 5: "SPCONV_E_NOMEM", 6: "SPCONV_E_HIP"}
-F32, F16, BF16, FP8 = 0, 1, 2, 3
+F32, F16, BF16, FP8, MXFP4 = 0, 1, 2, 3, 4
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
 _ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "relu6": ACT_RELU6}
 _DTYPES = {"f32": F32, "f16": F16}
-# element types of the 8-bit products, the router and the experts
-_OP_DTYPES = {"f32": F32, "f16": F16, "bf16": BF16, "fp8": FP8}
+# element types of the 8-bit and 4-bit products, norms, the router, the experts and sampling
+_OP_DTYPES = {"f32": F32, "f16": F16, "bf16": BF16, "fp8": FP8, "mxfp4": MXFP4}
 
 # Symbols declared in include/spconv.h.
 EXPORTED = ("spconv_plan_create", "spconv_run", "spconv_destroy", "spconv_last_error",
@@ -36,7 +36,9 @@ EXPORTED = ("spconv_plan_create", "spconv_run", "spconv_destroy", "spconv_last_e
             "spconv_dense_to_bcsr_blocked", "spconv_plan_create_dense_blocked", "spconv_plan_unpack_indexed",
             "spconv_plan_check", "spconv_plan_set_wait_limit", "spconv_plan_create_static",
             "spconv_plan_unpack_outer", "spconv_plan_run_kernel", "spconv_quantize_fp8", "spconv_linear_fp8",
-            "spconv_linear_fp8_workspace", "spconv_route", "spconv_experts_fp8", "spconv_experts_fp8_workspace")
+            "spconv_linear_fp8_workspace", "spconv_route", "spconv_experts_fp8", "spconv_experts_fp8_workspace",
+            "spconv_rms_norm", "spconv_quantize_mxfp4", "spconv_linear_mxfp4", "spconv_linear_mxfp4_workspace",
+            "spconv_sample", "spconv_sample_workspace")
 
 
 class SpconvError(RuntimeError):
@@ -164,6 +166,19 @@ def load_library(path: Optional[str] = None):
     lib.spconv_experts_fp8.argtypes = [vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp]
     lib.spconv_experts_fp8_workspace.restype = i32
     lib.spconv_experts_fp8_workspace.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+    f32 = ctypes.c_float
+    lib.spconv_rms_norm.restype = i32
+    lib.spconv_rms_norm.argtypes = [vp, i32, i64, vp, i32, i64, vp, i64, vp, i32, f32, vp, i32, i64, vp, vp, i32, i32, vp]
+    lib.spconv_quantize_mxfp4.restype = i32
+    lib.spconv_quantize_mxfp4.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+    lib.spconv_linear_mxfp4.restype = i32
+    lib.spconv_linear_mxfp4.argtypes = [vp, i32, i64, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, vp, i64, vp]
+    lib.spconv_linear_mxfp4_workspace.restype = i32
+    lib.spconv_linear_mxfp4_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.spconv_sample.restype = i32
+    lib.spconv_sample.argtypes = [vp, i32, i64, vp, i32, i32, vp, vp, vp, vp, f32, i32, f32, f32, vp, vp, i64, vp]
+    lib.spconv_sample_workspace.restype = i32
+    lib.spconv_sample_workspace.argtypes = [i32, i32, i32, ctypes.POINTER(i64)]
     if path is None:
         _lib = lib
         _bind_current_stream()
@@ -525,6 +540,69 @@ def spconv_experts_fp8_workspace(n, k, experts, hidden, inner) -> int:
     b = ctypes.c_int64()
     _check(load_library().spconv_experts_fp8_workspace(int(n), int(k), int(experts), int(hidden), int(inner),
                                                        ctypes.byref(b)))
+    return b.value
+
+
+def spconv_rms_norm(x, dtype, ldx, residual, residual_dtype, ldr, total, ldt, gain, gain_dtype, eps, y, y_dtype, ldy,
+                    q, scale, rows, cols, stream=None, check: bool = True):
+    """Queue the norm of rows, with the residual's addition and 8-bit codes where given."""
+    status = load_library().spconv_rms_norm(_devptr(x), _op_dtype(dtype), int(ldx), _devptr(residual),
+                                            _op_dtype(residual_dtype), int(ldr), _devptr(total), int(ldt),
+                                            _devptr(gain), _op_dtype(gain_dtype), float(eps), _devptr(y),
+                                            _op_dtype(y_dtype), int(ldy), _devptr(q), _devptr(scale), int(rows),
+                                            int(cols), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_quantize_mxfp4(x, dtype, ldx, rows, cols, q, scale, stream=None, check: bool = True):
+    """Queue the conversion of a matrix to 4-bit codes and powers of two."""
+    status = load_library().spconv_quantize_mxfp4(_devptr(x), _op_dtype(dtype), int(ldx), int(rows), int(cols),
+                                                  _devptr(q), _devptr(scale), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_linear_mxfp4(x, x_dtype, ldx, x_scale, w, w_scale, bias, act, y, y_dtype, n, cin, cout, workspace=None,
+                        workspace_bytes=0, stream=None, check: bool = True):
+    """Queue the dense layer y = act(x W^T + b) with a 4-bit weight."""
+    a = _ACTS[act] if isinstance(act, str) else int(act)
+    status = load_library().spconv_linear_mxfp4(_devptr(x), _op_dtype(x_dtype), int(ldx), _devptr(x_scale),
+                                                _devptr(w), _devptr(w_scale), _devptr(bias), a, _devptr(y),
+                                                _op_dtype(y_dtype), int(n), int(cin), int(cout), _devptr(workspace),
+                                                int(workspace_bytes), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_linear_mxfp4_workspace(x_dtype, n, cin, cout) -> int:
+    """Bytes of workspace that spconv_linear_mxfp4 needs."""
+    b = ctypes.c_int64()
+    _check(load_library().spconv_linear_mxfp4_workspace(_op_dtype(x_dtype), int(n), int(cin), int(cout),
+                                                        ctypes.byref(b)))
+    return b.value
+
+
+def spconv_sample(logits, dtype, ld, u, n, vocab, temperatures=None, top_ks=None, top_ps=None, min_ps=None,
+                  temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ids=None, workspace=None, workspace_bytes=0,
+                  stream=None, check: bool = True):
+    """Queue the choice of each row's next token."""
+    status = load_library().spconv_sample(_devptr(logits), _op_dtype(dtype), int(ld), _devptr(u), int(n), int(vocab),
+                                          _devptr(temperatures), _devptr(top_ks), _devptr(top_ps), _devptr(min_ps),
+                                          float(temperature), int(top_k), float(top_p), float(min_p), _devptr(ids),
+                                          _devptr(workspace), int(workspace_bytes), _stream(stream) or None)
+    if check:
+        _check(status)
+    return status
+
+
+def spconv_sample_workspace(dtype, n, vocab) -> int:
+    """Bytes of workspace that spconv_sample needs."""
+    b = ctypes.c_int64()
+    _check(load_library().spconv_sample_workspace(_op_dtype(dtype), int(n), int(vocab), ctypes.byref(b)))
     return b.value
 
 
