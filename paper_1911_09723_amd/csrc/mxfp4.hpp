@@ -43,6 +43,90 @@ __device__ __forceinline__ uint32_t codes8(const float *v, uint32_t power) {
     return power == 255 ? 0 : w;
 }
 
+// The same of eight values as they lie in memory, f32, f16 or bf16.  Largest
+// magnitudes of 16-bit values are found two at a time on their bits, and the
+// conversion takes the pairs as they are.
+template <typename T>
+struct Eight {
+    T v[8];
+};
+
+typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bh2 __attribute__((ext_vector_type(2)));
+
+// Eight neighbours from p, of which `left` exist; the others are zeros.
+template <typename T>
+__device__ __forceinline__ Eight<T> eight_tail(const T *p, int left, bool wide) {
+    struct __attribute__((aligned(16))) Piece {
+        T v[8];
+    };
+    Eight<T> r;
+    if (wide && left >= 8) {
+        const Piece a = *reinterpret_cast<const Piece *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            r.v[i] = a.v[i];
+        return r;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        r.v[i] = i < left ? p[i] : static_cast<T>(0.0f);
+    return r;
+}
+
+// The largest magnitude's bits so far, in a form of T's own: starts at 0.
+template <typename T>
+__device__ __forceinline__ uint32_t most_of(uint32_t most, const Eight<T> &e) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            most = max(most, magnitude(e.v[i]));
+    } else {
+        const u4 pairs = __builtin_bit_cast(u4, e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, most),
+                                                                          __builtin_bit_cast(us2, pairs[i] & 0x7fff7fffu)));
+    }
+    return most;
+}
+
+// That form as the byte that the block keeps.
+template <typename T>
+__device__ __forceinline__ uint32_t power_of_most(uint32_t most) {
+    if constexpr (sizeof(T) == 4) {
+        return power_of(most);
+    } else {
+        const uint16_t m = static_cast<uint16_t>(max(most & 0xffffu, most >> 16));
+        return power_of(__float_as_uint(static_cast<float>(__builtin_bit_cast(T, m))));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t codes8(const Eight<T> &e, uint32_t power) {
+    if constexpr (sizeof(T) == 4) {
+        return codes8(e.v, power);
+    } else {
+        const float scale = __uint_as_float(power ? power << 23 : 1u << 22);
+        struct Pairs {
+            uint32_t v[4];
+        } pairs = __builtin_bit_cast(Pairs, e);
+        uint32_t w = 0;
+        if constexpr (__is_same(T, _Float16)) {
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, pairs.v[0]), scale, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, pairs.v[1]), scale, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, pairs.v[2]), scale, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, pairs.v[3]), scale, 3);
+        } else {
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bh2, pairs.v[0]), scale, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bh2, pairs.v[1]), scale, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bh2, pairs.v[2]), scale, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bh2, pairs.v[3]), scale, 3);
+        }
+        return power == 255 ? 0 : w;
+    }
+}
+
 // p (16 x 16, f4 a lane) = c + A (16 rows x 128) B (16 columns x 128), 4-bit codes
 // with the scales of lane l in byte OP of sa and sb: lane l holds of each operand
 // row l % 16 a block of 32 channels (any, the same for both), of the result column

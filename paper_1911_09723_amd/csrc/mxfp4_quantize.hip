@@ -16,20 +16,22 @@ __global__ void __launch_bounds__(256) quantize4_rows(const T *x, int64_t ldx, i
         return;
     const T *xr = x + row * ldx;
     const int32_t l0 = part * U;
-    float v[U][8];
+    Eight<T> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t c = (l0 + u) * kLine4 + 8 * l;
-        load8_tail(xr + c, cols - c, wide, v[u]);
+        v[u] = eight_tail(xr + c, cols - c, wide);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (l0 + u >= lines)
             break;
-        uint32_t m = most8(v[u]);
+        uint32_t m = most_of(0, v[u]);
+        if constexpr (sizeof(T) == 2)
+            m = max(m & 0xffffu, m >> 16);
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
-        const uint32_t power = power_of(m);
+        const uint32_t power = power_of_most<T>(m);
         *reinterpret_cast<uint32_t *>(q + (static_cast<int64_t>(row) * lines + l0 + u) * 128 + 4 * l) = codes8(v[u], power);
         if ((l & 3) == 0)
             scale[(static_cast<int64_t>(l0 + u) * rows + row) * 8 + (l >> 2)] = static_cast<uint8_t>(power);

@@ -57,17 +57,12 @@ spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t
     return SPCONV_OK;
 }
 
-// A call's workspace: rows that the product's kernel does not quantise itself, as codes and
-// scales, then the sums of workgroups that share the input channels.
-struct LinearSpace {
-    int64_t rows, sums;
-};
-LinearSpace linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
-    if (n == 0 || cout == 0)
-        return {0, 0};
-    const bool as_is = x_dtype == SPCONV_MXFP4 || spconv::linear4_takes_rows(n, cin, cout);
-    const int64_t splits = spconv::linear4_splits(n, cin, cout), cells = static_cast<int64_t>(n) * ((cout + 3) / 4 * 4);
-    return {as_is ? 0 : code_bytes(n, cin) + align16(scale_bytes(n, cin)), splits > 1 ? splits * cells * 4 : 0};
+// A call's workspace: the codes and scales of rows that the product's kernel does not
+// quantise itself.
+int64_t linear_workspace(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t cout) {
+    if (n == 0 || cout == 0 || x_dtype == SPCONV_MXFP4 || spconv::linear4_takes_rows(n, cin, cout))
+        return 0;
+    return code_bytes(n, cin) + align16(scale_bytes(n, cin));
 }
 
 spconv_status check_sample(spconv_dtype dtype, int32_t n, int32_t vocab) {
@@ -186,10 +181,8 @@ spconv_status spconv_linear_mxfp4_workspace(spconv_dtype x_dtype, int32_t n, int
         return set_error(SPCONV_E_ARG, "bytes is NULL");
     *bytes = 0;
     const spconv_status st = check_linear(x_dtype, n, cin, cout);
-    if (st == SPCONV_OK) {
-        const LinearSpace space = linear_workspace(x_dtype, n, cin, cout);
-        *bytes = space.rows + space.sums;
-    }
+    if (st == SPCONV_OK)
+        *bytes = linear_workspace(x_dtype, n, cin, cout);
     return st;
 }
 
@@ -219,8 +212,7 @@ spconv_status spconv_linear_mxfp4(const void *x, spconv_dtype x_dtype, int64_t l
     if (!aligned(x, codes ? 16 : size_of(x_dtype)) || !aligned(w, 16) || !aligned(y, size_of(y_dtype)) ||
         !aligned(x_scale, 16) || !aligned(w_scale, 16) || !aligned(bias, 4) || !aligned(workspace, 16))
         return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size, codes, scales and the workspace to 16 bytes");
-    const LinearSpace space = linear_workspace(x_dtype, n, cin, cout);
-    const int64_t need = space.rows + space.sums;
+    const int64_t need = linear_workspace(x_dtype, n, cin, cout);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return set_error(SPCONV_E_ARG, "the workspace is smaller than spconv_linear_mxfp4_workspace says");
     const Range in[] = {{x, codes ? code_bytes(n, cin) : span(n, cin, ldx, size_of(x_dtype))},
@@ -247,8 +239,7 @@ spconv_status spconv_linear_mxfp4(const void *x, spconv_dtype x_dtype, int64_t l
     a.cout = cout;
     a.lines = lines_of(cin);
     clamp_of(act, a.lo, a.hi);
-    a.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + space.rows);
-    if (space.rows > 0) {
+    if (need > 0) {
         uint8_t *q = static_cast<uint8_t *>(workspace), *scale = q + code_bytes(n, cin);
         const hipError_t e = spconv::launch_quantize_mxfp4(x, x_dtype, ldx, n, cin, q, scale, s);
         if (e != hipSuccess)

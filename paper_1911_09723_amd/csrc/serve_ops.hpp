@@ -28,6 +28,9 @@ struct NormArgs {
 // type: of x; residual and gain are of that type or (residual32, gain32) in f32.
 hipError_t launch_norm(NormArgs a, int32_t type, bool residual32, bool gain32, hipStream_t stream);
 
+// Rows kept as 4-bit codes (spconv_dtype).
+enum : int32_t { kMxfp4 = 4 };
+
 // Lines of 256 channels, which are 128 bytes of 4-bit codes.
 inline int32_t lines_of(int64_t channels) { return static_cast<int32_t>((channels + 255) / 256); }
 
@@ -44,15 +47,12 @@ struct Linear4Args {
     const uint8_t *ws;    // [lines][cout][8]
     const float *bias;    // [cout] or null
     void *y;
-    float *partial;       // [splits][n][cout rounded up to 4] where workgroups share the input channels
     int32_t x_type, y_type;
     int32_t n, cin, cout, lines;
     float lo, hi;
 };
 // Whether rows that are not quantised yet are quantised inside the product's kernel.
 bool linear4_takes_rows(int32_t n, int32_t cin, int32_t cout);
-// How many workgroups share the input channels of a tile; above 1 the call needs `partial`.
-int32_t linear4_splits(int32_t n, int32_t cin, int32_t cout);
 hipError_t launch_linear_mxfp4(const Linear4Args &a, hipStream_t stream);
 
 // Tokens [n] from logits [n][vocab] (row stride ld elements).

@@ -102,6 +102,17 @@ def test_linear(n, cin, cout, dtype):
     _check(layer, x, layer.run(x), dtype)
 
 
+@pytest.mark.parametrize("n,cin,cout,dtype", [(9, 2300, 33, "bf16"), (3, 1000, 5000, "f32"), (8, 500, 4100, "f16"), (13, 300, 70000, "f16"),
+                                              (20, 300, 9000, "bf16"), (50, 300, 33000, "bf16"), (300, 600, 2048, "f32"),
+                                              (300, 4200, 4096, "bf16"), (290, 500, 4100, "f16"), (1200, 2100, 4000, "bf16"),
+                                              (1200, 300, 4001, "f16"), (2600, 300, 4100, "bf16"), (2600, 513, 4096, "f32")])
+def test_linear_of_every_tile(n, cin, cout, dtype):
+    note("linear4 %d x %d -> %d %s" % (n, cin, cout, dtype))
+    layer = _layer(cout, cin, 3, True, "relu6" if n % 2 else "none")
+    x = _draw(n, cin, dtype, 4)
+    _check(layer, x, layer.run(x), dtype)
+
+
 @pytest.mark.parametrize("n,cin,cout", [(1, 1024, 100), (20, 2048, 333), (40, 512, 512), (130, 1536, 264), (600, 1024, 520),
                                         (1100, 512, 1030), (64, 16384, 128), (2100, 256, 2050)])
 def test_exact_sums(n, cin, cout):
