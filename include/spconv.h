@@ -471,8 +471,9 @@ SPCONV_API spconv_status spconv_rms_norm(const void *x, spconv_dtype dtype, int6
  * exceeds u times their sum.  t = 0 takes the first of the order.  A token whose
  * logit is -infinity or NaN is off: never taken, of no weight; +infinity counts as the
  * largest finite float.  A row without a token that is on gets -1.
- * Weights are 64-bit, in their sums multiples of 2^-42 of the largest: the choice
- * does not hang on the order of additions, and is the same in every call.
+ * Weights are 64-bit (4e-14 off), in their sums multiples of 2^-42 of the largest
+ * (of all, or of 8192 neighbours): the choice does not hang on the order of
+ * additions nor on the other rows, and is the same in every call.
  *   logits  device, [n][vocab] of dtype (F32, F16 or BF16), row stride ld >= vocab elements
  *   u       device, n floats in [0, 1); below 0 or NaN counts as 0, 1 and above as the
  *           largest float below 1

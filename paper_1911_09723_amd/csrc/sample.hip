@@ -22,22 +22,29 @@
 // added up.  A bin with more than the list holds goes digit by digit through the
 // keys.
 //
-// Rows of up to 8192 tokens, or 32768 where all rows keep few: one workgroup a row,
-// which keeps it in LDS.  Longer rows are cut into chunks of 8192 neighbours, one a workgroup, so that a few
-// rows fill the card; a launch ends where every chunk's part is needed:
+// Rows of up to 8192 tokens: one workgroup a row, which keeps it in LDS.  Longer
+// rows are cut into chunks of 8192 neighbours, one a workgroup, so that a few rows
+// fill the card; a launch ends where every chunk's part is needed:
 //   A  each chunk's largest key, the largest of each 32 tokens (a segment), and,
 //      where nothing is filtered, the sum of its weights;
 //   B  rows without a filter: the chunk that holds the border, and the token in it.
-//      Up to 1024 tokens kept (k): the k-th largest of the segments' keys bounds the
-//      k-th largest key from below, so that only the segments above it are read
+//      Few tokens kept (k): the k-th largest of the segments' keys bounds the k-th
+//      largest key from below, so that only the segments above it are read
 //      again.  Else, for all chunks: sums (min_p) or the histogram;
 //   C  each chunk adds up what is above the border's bin and lists what is in it;
 //   D  the border in the list, the chunk, the token.
 // k above 1024 together with p, and longer lists than 8192, go to one workgroup that
 // walks over the whole row.
+//
+// What bounds it.  64 x 131072 in bf16 (16.8 MB, 3.3 us at a copy's rate), on the device alone: t = 0
+// 8.8 us; no filter 23, of it 9 the exponentials (25 64-bit operations each); k = 50 20, of it 13
+// the steps of B, one after the other, each some loads or a few LDS accesses and barriers long; p =
+// 0.9 63: A 7, B 17.5 (exponentials and LDS atomics), C 18.5, D 19.7.  One row of 4000: 8.4 to
+// 9.1, with p 14.6.  Steps one after the other are why a workgroup has 512 threads and not 1024
+// (each thread's share of such a step is done by twice as many: k = 50 of 4000 took 14 us).
 #include <algorithm>
 
-#include "fp8_product.hpp"
+#include "fp8.hpp"
 #include "serve_ops.hpp"
 
 namespace spconv {
@@ -51,7 +58,6 @@ constexpr int kBins = 2048;       // of a histogram
 constexpr int kThreads = 512;     // of a workgroup but in A
 constexpr int kWaves = kThreads / 64;
 constexpr int kChunk = 8192;
-constexpr int kShort = 32768;     // longest row that LDS holds
 constexpr int kSegments = 256;    // of a chunk: threads in A, 32 tokens each
 constexpr int kFew = 1024;        // most tokens that a list in LDS holds
 constexpr int kSorted = 128;      // most of them that are sorted at once
@@ -92,6 +98,11 @@ __device__ __forceinline__ void load_logits(const T *p, int left, float *v) {
 
 enum Mode { kGreedy, kAll, kLeast, kFewKept, kShare, kCount, kDigits };
 
+// Whether the first k of a row are listed in LDS.  Alone, more than 512 take less as a histogram
+// (1000 of 131072, one row, 39 us and 99; 256 x 50001 83 and 95); together with a share, a list is
+// what there is but for the walk over the whole row (64 x 131072, k = 2000 and p = 0.9: 336 us).
+__host__ __device__ __forceinline__ bool few_kept(int32_t k, bool share) { return k <= (share ? kFew : 512); }
+
 // A number that stays in scalar registers: else each use of it would be moved to vector registers.
 __device__ __forceinline__ double scalar(double v) {
     asm("" : "+s"(v));
@@ -131,7 +142,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs &a, int32_t row) {
     const bool some = r.top_k < a.vocab, share = r.top_p < 1;
     r.mode = !(t > 0)            ? kGreedy
              : !some && !share   ? r.min_p > 0 ? kLeast : kAll
-             : some && r.top_k <= kFew ? kFewKept
+             : some && few_kept(r.top_k, share) ? kFewKept
              : !some             ? kShare
              : !share            ? kCount
                                  : kDigits;
@@ -291,9 +302,8 @@ struct Found {
     double target;
 };
 
-// LDS of all kernels but A.
-struct Shared {
-    Sum bins[kBins];
+// LDS of all kernels but A: what finds borders, ...
+struct Common {
     Sum part[kWaves];
     Found found;
     uint32_t count;
@@ -301,13 +311,33 @@ struct Shared {
         int32_t first;
         Sum before;
     } at;
+};
+struct OneRow : Common {
+    Sum bins[kBins];
     uint64_t few[kFew];
     uint32_t rank[kFew];
 };
 
+// ... or a chunk with the chunks' sums.
+struct Shared : Common {
+    union {
+        struct {
+            Sum bins[kBins];
+            uint64_t few[kFew];
+            uint32_t rank[kFew];
+        };
+        struct {
+            Sum sums[kMostTokens / kChunk];
+            double mass[kMostTokens / kChunk], factor[kMostTokens / kChunk];
+            __attribute__((aligned(16))) float held[kChunk];
+        };
+    };
+};
+
 // The first bin from above (and not empty) at which the running sum reaches a number, or passes it: k,
 // or the share p of all bins where p < 1.
-__device__ __forceinline__ Found find(Shared &sh, const Sum *bins, double k, double p, bool pass = false) {
+template <class S>
+__device__ __forceinline__ Found find(S &sh, const Sum *bins, double k, double p, bool pass = false) {
     constexpr int kOwn = kBins / kThreads;
     if (threadIdx.x == 0)
         sh.found = {-1, 0, 0, 0};
@@ -365,7 +395,8 @@ __device__ __forceinline__ uint32_t place_in(uint32_t *total, uint32_t count) {
 // Puts the first m (at most kSorted) of sh.few, different where not 0, in order, the largest first:
 // each counts the larger ones, blocks of 64 by wavefronts, which share the others.  (A network of
 // exchanges, whose steps wait for each other, took 1.8 us for 64.)
-__device__ __forceinline__ void sort_few(Shared &sh, int32_t m) {
+template <class S>
+__device__ __forceinline__ void sort_few(S &sh, int32_t m) {
     if (m < 2)
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -396,8 +427,8 @@ __device__ __forceinline__ void sort_few(Shared &sh, int32_t m) {
 // Of m values in sh.few (different where not 0) the first, from the largest on, at which the running
 // weight(value) reaches `target`, or passes it; the least of them where a rounding leaves it short.
 // More than can be sorted at once are narrowed down by their digits.  Uses sh.few and sh.bins up.
-template <class Weight>
-__device__ __forceinline__ uint64_t border_of_few(Shared &sh, int32_t m, double target, bool pass, Weight weight) {
+template <class S, class Weight>
+__device__ __forceinline__ uint64_t border_of_few(S &sh, int32_t m, double target, bool pass, Weight weight) {
     constexpr int kOwn = kFew / kThreads;
     const int32_t t = static_cast<int32_t>(threadIdx.x);
     if (m > kSorted) {
@@ -466,8 +497,8 @@ __device__ __forceinline__ uint64_t border_of_few(Shared &sh, int32_t m, double 
 // where it never does, the least key that has the prefix.  shift: bits below the ones that all
 // keys have in common (prefix).
 // enough: stops where so few weights (counts) are up to the end of a bin, at its least key.
-template <class Each>
-__device__ __forceinline__ uint64_t least_key(Shared &sh, double target, uint64_t prefix, int shift, Sum enough, Each each) {
+template <class S, class Each>
+__device__ __forceinline__ uint64_t least_key(S &sh, double target, uint64_t prefix, int shift, Sum enough, Each each) {
     Sum above = 0;
     while (shift > 0) {
         const int width = min(shift, 11), to = shift - width;
@@ -494,8 +525,8 @@ __device__ __forceinline__ uint64_t least_key(Shared &sh, double target, uint64_
 // ones that earlier filters kept: the first, from the largest on, at which the running weight(key)
 // reaches k, or the share p of all where p < 1; 0 where all are kept.  `list(test)` appends the
 // keys of those tokens that pass to sh.few, up to kFew, and counts all.
-template <class Walk, class List, class Weight>
-__device__ __forceinline__ uint64_t border_of(Shared &sh, float most, double k, double p, Walk walk, List list, Weight weight) {
+template <class S, class Walk, class List, class Weight>
+__device__ __forceinline__ uint64_t border_of(S &sh, float most, double k, double p, Walk walk, List list, Weight weight) {
     if (threadIdx.x == 0)
         sh.count = 0;
     clear(sh.bins, kBins);
@@ -532,9 +563,9 @@ __device__ __forceinline__ uint64_t border_of(Shared &sh, float most, double k, 
 // from `first` on, of which token i adds kept(i); at the last one's end it does.  A thread adds up
 // a run of them, an odd number (LDS is then read without conflicts), and one wavefront looks
 // through the run that holds the border.
-template <class Kept>
+template <class S, class Kept>
 __device__ __forceinline__ void pick(const SampleArgs &a, int32_t row, int32_t first, int32_t count, Sum before, double border,
-                                     Shared &sh, Kept kept) {
+                                     S &sh, Kept kept) {
     const int32_t each = ((count + kThreads - 1) / kThreads) | 1, i0 = static_cast<int32_t>(threadIdx.x) * each;
     const int32_t own = min(max(count - i0, 0), each);
     Sum mine = 0, run;
@@ -566,7 +597,8 @@ __device__ __forceinline__ void pick(const SampleArgs &a, int32_t row, int32_t f
 
 // The token from m keys in sh.few, among them the first k of the row: in their order, where each
 // filter keeps a start of what the one before kept, then by index.
-__device__ __forceinline__ void pick_few(const SampleArgs &a, int32_t row, const Row &r, int32_t m, float most, Shared &sh) {
+template <class S>
+__device__ __forceinline__ void pick_few(const SampleArgs &a, int32_t row, const Row &r, int32_t m, float most, S &sh) {
     const int32_t t = static_cast<int32_t>(threadIdx.x);
     if (m <= kSorted) {
         sort_few(sh, m);
@@ -638,13 +670,13 @@ __device__ __forceinline__ void pick_few(const SampleArgs &a, int32_t row, const
 
 // One row in one workgroup; held: LDS that takes the row, or null: then it is read anew for each
 // step.
-template <typename T, bool HELD>
-__device__ __forceinline__ void whole_row(const SampleArgs &a, int32_t row, const Row &r, Shared &sh, float *held) {
+template <typename T, bool HELD, class S>
+__device__ __forceinline__ void whole_row(const SampleArgs &a, int32_t row, const Row &r, S &sh, float *held) {
     const T *l = static_cast<const T *>(a.logits) + row * a.ld;
     const int32_t t = static_cast<int32_t>(threadIdx.x);
     float top = -INFINITY;  // of this thread's groups of eight neighbours
     int32_t token = 0;
-#pragma unroll 2
+#pragma unroll 4
     for (int32_t i = t * 8; i < a.vocab; i += kThreads * 8) {
         float v[8];
         load_logits(l + i, a.vocab - i, v);
@@ -779,8 +811,8 @@ __device__ __forceinline__ void whole_row(const SampleArgs &a, int32_t row, cons
 // row, 256 rows at a time.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_short(SampleArgs a) {
-    __shared__ Shared sh;
-    extern __shared__ __attribute__((aligned(16))) float held[];
+    __shared__ OneRow sh;
+    __shared__ __attribute__((aligned(16))) float held[kChunk];
     whole_row<T, true>(a, blockIdx.x, row_of(a, blockIdx.x), sh, held);
 }
 
@@ -842,18 +874,24 @@ __global__ void __launch_bounds__(kSegments) sample_chunks(SampleArgs a) {
         s.sums[chunk] = sum;
 }
 
-// A chunk's logits to LDS, as they count.
+// A chunk's logits, as they count: 8 neighbours of each piece of 4096.
+constexpr int kPieces = kChunk / kThreads / 8;
 template <typename T>
-__device__ __forceinline__ void hold(const SampleArgs &a, int32_t row, int32_t chunk, float *held) {
-    float v[kChunk / kThreads / 8][8];
+__device__ __forceinline__ void load_chunk(const SampleArgs &a, int32_t row, int32_t chunk, float (&v)[kPieces][8]) {
 #pragma unroll
-    for (int j = 0; j < kChunk / kThreads / 8; ++j) {
+    for (int j = 0; j < kPieces; ++j) {
         const int32_t i = chunk * kChunk + (j * kThreads + static_cast<int32_t>(threadIdx.x)) * 8;
         load_logits(static_cast<const T *>(a.logits) + row * a.ld + i, a.vocab - i, v[j]);
     }
+}
+
+template <typename T>
+__device__ __forceinline__ void hold(const SampleArgs &a, int32_t row, int32_t chunk, float *held) {
+    float v[kPieces][8];
+    load_chunk<T>(a, row, chunk, v);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kChunk / kThreads / 8; ++j) {
+    for (int j = 0; j < kPieces; ++j) {
         f4 *to = reinterpret_cast<f4 *>(held) + (j * kThreads + threadIdx.x) * 2;
         to[0] = f4{v[j][0], v[j][1], v[j][2], v[j][3]};
         to[1] = f4{v[j][4], v[j][5], v[j][6], v[j][7]};
@@ -863,14 +901,14 @@ __device__ __forceinline__ void hold(const SampleArgs &a, int32_t row, int32_t c
 
 // The first token of a row that kept(logit, token) keeps, for u = 0.
 template <typename T, class Kept>
-__device__ __forceinline__ void pick_first(const SampleArgs &a, int32_t row, int32_t chunks, Shared &sh, float *held, Kept kept) {
+__device__ __forceinline__ void pick_first(const SampleArgs &a, int32_t row, int32_t chunks, Shared &sh, Kept kept) {
 #pragma unroll 1
     for (int32_t c = 0; c < chunks; ++c) {
-        hold<T>(a, row, c, held);
+        hold<T>(a, row, c, sh.held);
         uint64_t first = 0;  // the smaller the token, the larger
 #pragma unroll 1
         for (int32_t i = threadIdx.x; i < kChunk && !first; i += kThreads)
-            first = kept(held[i], c * kChunk + i) ? kMostTokens - (c * kChunk + i) : 0;
+            first = kept(sh.held[i], c * kChunk + i) ? kMostTokens - (c * kChunk + i) : 0;
         first = most_block<kWaves>(first, sh.part);
         if (first) {
             if (threadIdx.x == 0)
@@ -883,9 +921,9 @@ __device__ __forceinline__ void pick_first(const SampleArgs &a, int32_t row, int
 // The token from the chunks' sums of kept weights, in units of the row's largest.
 template <typename T, class Kept>
 __device__ __forceinline__ void pick_by_sums(const SampleArgs &a, int32_t row, const Row &r, const Sum *sums, int32_t chunks,
-                                             Shared &sh, float *held, Kept kept) {
+                                             Shared &sh, Kept kept) {
     if (r.u == 0) {
-        pick_first<T>(a, row, chunks, sh, held, kept);
+        pick_first<T>(a, row, chunks, sh, kept);
         return;
     }
     Sum total = 0, before = 0;
@@ -895,19 +933,19 @@ __device__ __forceinline__ void pick_by_sums(const SampleArgs &a, int32_t row, c
     int32_t chunk = 0;
     while (chunk < chunks - 1 && !(static_cast<double>(before + sums[chunk]) > border))
         before += sums[chunk++];
-    hold<T>(a, row, chunk, held);
-    pick(a, row, chunk * kChunk, kChunk, before, border, sh, [&](int32_t i) { return kept(held[i - chunk * kChunk], i); });
+    hold<T>(a, row, chunk, sh.held);
+    pick(a, row, chunk * kChunk, kChunk, before, border, sh, [&](int32_t i) { return kept(sh.held[i - chunk * kChunk], i); });
 }
 
 // Rows without a filter: chunks' sums are in units of their own largest weight.
 template <typename T>
 __device__ __forceinline__ void pick_all(const SampleArgs &a, int32_t row, const Row &r, const Space &s, int32_t chunks, float most,
-                                         Shared &sh, float *held) {
+                                         Shared &sh) {
     if (r.u == 0) {
-        pick_first<T>(a, row, chunks, sh, held, [&](float v, int32_t) { return v > -INFINITY && weighs(v, most, r); });
+        pick_first<T>(a, row, chunks, sh, [&](float v, int32_t) { return v > -INFINITY && weighs(v, most, r); });
         return;
     }
-    double *mass = reinterpret_cast<double *>(sh.bins), *factor = mass + 128;
+    double *mass = sh.mass, *factor = sh.factor;
     if (threadIdx.x < static_cast<unsigned>(chunks)) {
         const uint64_t best = s.best[threadIdx.x];
         const double f = best ? weight_of(logit_of(best), most, r) * 0x1p-42 : 0.0;
@@ -928,9 +966,9 @@ __device__ __forceinline__ void pick_all(const SampleArgs &a, int32_t row, const
     const double own = static_cast<double>(s.sums[chunk]);
     const double rest = fmin((border - before) / factor[chunk], own * (1 - 0x1p-52));
     const float top = logit_of(s.best[chunk]);
-    hold<T>(a, row, chunk, held);
+    hold<T>(a, row, chunk, sh.held);
     pick(a, row, chunk * kChunk, kChunk, 0, rest, sh, [&](int32_t i) -> Sum {
-        const float v = held[i - chunk * kChunk];
+        const float v = sh.held[i - chunk * kChunk];
         const Sum w = units(weight_of(v, top, r), r);
         return v > -INFINITY ? w : 0;
     });
@@ -938,12 +976,40 @@ __device__ __forceinline__ void pick_all(const SampleArgs &a, int32_t row, const
 
 // Up to 1024 tokens kept: the segments that can hold them, and their tokens.
 template <typename T>
-__device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, const Row &r, const Space &s, int32_t chunks, float most, Shared &sh) {
-    const int32_t segments = chunks * kSegments;
+__device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, const Row &r, const Space &s, int32_t chunks, Shared &sh) {
+    const int32_t segments = chunks * kSegments, t = static_cast<int32_t>(threadIdx.x);
+    uint64_t head[8];  // of the first 4096 segments, asked for before the maximum is known
+    auto eight = [&](int32_t g0, uint64_t (&k)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            k[j] = g0 + t + j * kThreads < segments ? s.segments[g0 + t + j * kThreads] : 0;
+    };
+    eight(0, head);
+    auto keys = [&](auto f) {  // f(key, segment) by all threads as often
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            f(head[j], t + j * kThreads);
+#pragma unroll 1
+        for (int32_t g0 = kThreads * 8; g0 < segments; g0 += kThreads * 8) {
+            uint64_t k[8];
+            eight(g0, k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                f(k[j], g0 + t + j * kThreads);
+        }
+    };
+    const uint64_t best = best_of(s, chunks);
+    if (best == 0) {
+        if (t == 0)
+            a.ids[row] = -1;
+        return;
+    }
+    const float most = logit_of(best);
     clear(sh.bins, kBins);
-    for (int32_t g = threadIdx.x; g < segments; g += kThreads)
-        if (const uint64_t k = s.segments[g])
+    keys([&](uint64_t k, int32_t) {
+        if (k)
             atomicAdd(&sh.bins[bin_of(logit_of(k), most)], Sum(1));
+    });
     __syncthreads();
     const Found f = find(sh, sh.bins, r.top_k, 1.0);
     uint64_t least = 0;  // with fewer segments that have a token than k
@@ -951,22 +1017,24 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
     if (f.bin >= 0 && f.upto > kFew) {  // more than 1024 up to the end of that bin
         bin = -1;
         least = least_key(sh, r.top_k, 0, 32 + kIndexBits, kFew, [&](auto g) {
-            for (int32_t i = threadIdx.x; i < segments; i += kThreads)
-                if (const uint64_t k = s.segments[i])
+            keys([&](uint64_t k, int32_t) {
+                if (k)
                     g(k, Sum(1));
+            });
         });
     }
     uint32_t *ids = sh.rank;  // (until the list is sorted)
     if (threadIdx.x == 0)
         sh.count = 0;
     __syncthreads();
-    for (int32_t g = threadIdx.x; g < segments; g += kThreads) {
-        const uint64_t k = s.segments[g];
+    keys([&](uint64_t k, int32_t g) {
         const bool in = k && k >= least && bin_of(logit_of(k), most) >= bin;
-        const uint32_t at = place_in(&sh.count, in);
-        if (in)
-            ids[at] = g;
-    }
+        if (__any(in)) {
+            const uint32_t at = place_in(&sh.count, in);
+            if (in)
+                ids[at] = g;
+        }
+    });
     __syncthreads();
     const int32_t few = static_cast<int32_t>(sh.count);
     // f(eight logits, their first token) for the pieces of these segments, all threads as often, four
@@ -1043,13 +1111,16 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_rows(SampleArgs a) {
     __shared__ Shared sh;
-    __shared__ __attribute__((aligned(16))) float held[kChunk];
     const int32_t row = blockIdx.y, chunk = blockIdx.x, chunks = chunks_of(a.vocab);  // (one workgroup where it does all)
     const Row r = row_of(a, row);
     const bool every = r.mode == kLeast || r.mode == kShare || r.mode == kCount;
     if (chunk > 0 && !every)
         return;
     const Space s = space_of(a, row);
+    if (r.mode == kFewKept) {
+        pick_segments<T>(a, row, r, s, chunks, sh);
+        return;
+    }
     const uint64_t best = best_of(s, chunks);
     if (best == 0 || r.mode == kGreedy) {
         if (chunk == 0 && threadIdx.x == 0)
@@ -1058,30 +1129,28 @@ __global__ void __launch_bounds__(kThreads) sample_rows(SampleArgs a) {
     }
     const float most = logit_of(best);
     if (r.mode == kAll) {
-        pick_all<T>(a, row, r, s, chunks, most, sh, held);
-        return;
-    }
-    if (r.mode == kFewKept) {
-        pick_segments<T>(a, row, r, s, chunks, most, sh);
+        pick_all<T>(a, row, r, s, chunks, most, sh);
         return;
     }
     if (r.mode == kDigits)
         return;
-    hold<T>(a, row, chunk, held);
+    float v[kPieces][8];
+    load_chunk<T>(a, row, chunk, v);
     clear(sh.bins, kBins);
     Sum sum = 0;
-#pragma unroll 4
-    for (int32_t i = threadIdx.x; i < kChunk; i += kThreads) {
-        const float v = held[i];
-        const double w = weight_of(v, most, r);
-        const Sum u = r.mode == kCount ? Sum(1) : units(w, r);
-        if (v > -INFINITY && u) {
-            if (r.mode != kLeast)
-                atomicAdd(&sh.bins[bin_of(v, most)], u);
-            else if (w >= r.min_p)
-                sum += u;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double w = weight_of(v[j][e], most, r);
+            const Sum u = r.mode == kCount ? Sum(1) : units(w, r);
+            if (v[j][e] > -INFINITY && u) {
+                if (r.mode != kLeast)
+                    atomicAdd(&sh.bins[bin_of(v[j][e], most)], u);
+                else if (w >= r.min_p)
+                    sum += u;
+            }
         }
-    }
     if (r.mode == kLeast) {
         sum = sum_block<kWaves>(sum, sh.part);
         if (threadIdx.x == 0)
@@ -1098,7 +1167,6 @@ __global__ void __launch_bounds__(kThreads) sample_rows(SampleArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_lists(SampleArgs a) {
     __shared__ Shared sh;
-    __shared__ __attribute__((aligned(16))) float held[kChunk];
     const int32_t row = blockIdx.y, chunk = blockIdx.x, chunks = gridDim.x;
     const Row r = row_of(a, row);
     if (r.mode != kShare && r.mode != kCount)
@@ -1108,45 +1176,45 @@ __global__ void __launch_bounds__(kThreads) sample_lists(SampleArgs a) {
     if (best == 0)
         return;
     const float most = logit_of(best);
+    float v[kPieces][8];
+    load_chunk<T>(a, row, chunk, v);
     const Found f = find(sh, s.bins, r.top_k, r.top_p);
-    hold<T>(a, row, chunk, held);
     Sum sum = 0, run;
-    uint32_t mine = 0;
-#pragma unroll 1
-    for (int32_t i = threadIdx.x; i < kChunk; i += kThreads) {
-        const float v = held[i];
-        const int b = v > -INFINITY ? bin_of(v, most) : -2;
-        if (b > f.bin) {
-            const double w = weight_of(v, most, r);
-            sum += w >= r.min_p ? units(w, r) : 0;
+    uint32_t hits = 0;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int b = v[j][e] > -INFINITY ? bin_of(v[j][e], most) : -2;
+            if (b > f.bin) {
+                const double w = weight_of(v[j][e], most, r);
+                sum += w >= r.min_p ? units(w, r) : 0;
+            }
+            hits |= static_cast<uint32_t>(b == f.bin) << (j * 8 + e);
         }
-        mine += b == f.bin;
-    }
     sum = sum_block<kWaves>(sum, sh.part);
     if (threadIdx.x == 0)
         s.sums[chunk] = sum;
-    const uint32_t all = static_cast<uint32_t>(sum_block<kWaves>(mine, sh.part, &run));
+    const uint32_t mine = __popc(hits), all = static_cast<uint32_t>(sum_block<kWaves>(mine, sh.part, &run));
     if (threadIdx.x == 0)
         sh.count = all ? atomicAdd(s.count, all) : 0;
     __syncthreads();
     uint32_t at = sh.count + static_cast<uint32_t>(run) - mine;
-    if (mine)
-#pragma unroll 1
-        for (int32_t i = threadIdx.x; i < kChunk; i += kThreads) {
-            const float v = held[i];
-            if (v > -INFINITY && bin_of(v, most) == f.bin) {
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (hits >> (j * 8 + e) & 1) {
                 if (at < kList)
-                    s.list[at] = key_of(v, chunk * kChunk + i);
+                    s.list[at] = key_of(v[j][e], chunk * kChunk + (j * kThreads + static_cast<int32_t>(threadIdx.x)) * 8 + e);
                 ++at;
             }
-        }
 }
 
 // D, a workgroup a row
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_borders(SampleArgs a) {
     __shared__ Shared sh;
-    __shared__ __attribute__((aligned(16))) float held[kChunk];
     const int32_t row = blockIdx.x, chunks = chunks_of(a.vocab);
     const Row r = row_of(a, row);
     if (r.mode == kGreedy || r.mode == kAll || r.mode == kFewKept)
@@ -1167,7 +1235,7 @@ __global__ void __launch_bounds__(kThreads) sample_borders(SampleArgs a) {
         return l > -INFINITY && key_of(l, token) >= least ? w : 0;
     };
     if (r.mode == kLeast) {
-        pick_by_sums<T>(a, row, r, s.sums, chunks, sh, held, kept);
+        pick_by_sums<T>(a, row, r, s.sums, chunks, sh, kept);
         return;
     }
     const Found f = find(sh, s.bins, r.top_k, r.top_p);
@@ -1197,7 +1265,7 @@ __global__ void __launch_bounds__(kThreads) sample_borders(SampleArgs a) {
             least = least > low ? least : low;
         }
     }
-    Sum *sums = sh.bins;
+    Sum *sums = sh.sums;
     for (int32_t c = threadIdx.x; c < chunks; c += kThreads)
         sums[c] = s.sums[c];
     __syncthreads();
@@ -1208,24 +1276,20 @@ __global__ void __launch_bounds__(kThreads) sample_borders(SampleArgs a) {
             atomicAdd(&sums[token / kChunk], w);
     }
     __syncthreads();
-    pick_by_sums<T>(a, row, r, sums, chunks, sh, held, kept);
+    pick_by_sums<T>(a, row, r, sums, chunks, sh, kept);
 }
 
 template <typename T>
 hipError_t launch(const SampleArgs &a, hipStream_t stream) {
     const int32_t chunks = chunks_of(a.vocab);
-    // rows that end in B: a small k, t = 0, no filter
-    const bool few = !a.top_ks && a.top_k > 0 && a.top_k <= kFew;
-    const bool greedy = !a.temperatures && !(a.temperature > 0);
-    const bool all = !a.top_ks && (a.top_k == 0 || a.top_k >= a.vocab) && !a.top_ps && a.top_p >= 1 && !a.min_ps && !(a.min_p > 0);
-    if (chunks == 1 || ((few || greedy) && a.vocab <= kShort)) {
-        static std::atomic<uint64_t> done{0};
-        const hipError_t ready = allow_lds(sample_short<T>, kShort * 4, done);
-        if (ready != hipSuccess)
-            return ready;
-        sample_short<T><<<a.n, kThreads, chunks * kChunk * 4, stream>>>(a);
+    if (chunks == 1) {
+        sample_short<T><<<a.n, kThreads, 0, stream>>>(a);
         return hipGetLastError();
     }
+    // rows that end in B: a small k, t = 0, no filter
+    const bool few = !a.top_ks && a.top_k > 0 && few_kept(a.top_k, !a.top_ps && a.top_p < 1);
+    const bool greedy = !a.temperatures && !(a.temperature > 0);
+    const bool all = !a.top_ks && (a.top_k == 0 || a.top_k >= a.vocab) && !a.top_ps && a.top_p >= 1 && !a.min_ps && !(a.min_p > 0);
     for (int32_t row = 0; row < a.n; row += 32768) {  // a grid's second axis ends at 65535
         SampleArgs part = a;
         const int32_t rows = std::min(a.n - row, 32768);
