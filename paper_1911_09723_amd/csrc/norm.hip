@@ -9,7 +9,8 @@
 //
 // One pass: a row stays in registers between its sum of squares and its
 // results, 8 neighbouring values a thread and piece, so that 16 lanes hold a
-// block of 128.
+// block of 128.  What bounds it is traffic, below some MB the launch and one wait for
+// the row's loads (1 x 1280: 3.9 us).
 #include <type_traits>
 
 #include "fp8.hpp"
@@ -18,36 +19,68 @@
 namespace spconv {
 namespace {
 
-constexpr int kXcds = 8;
-
 struct None {};
+
+// A piece of 16 or 8 bytes, past the caches where `stream`: of a long call little is still there
+// when the next one reads it, and it takes room from what is read.  bf16 with residual and codes,
+// us, through the caches and past them: 8192 x 4096 52.2 and 46.3 (loads kept: 47.9), 2048 x 4096
+// 16.6 and 14.4, 1024 x 4096 9.6 and 10.3.
+template <typename V>
+__device__ __forceinline__ void put(V *p, V v, bool stream) {
+    if (stream)
+        __builtin_nontemporal_store(v, p);
+    else
+        *p = v;
+}
 
 // `left` (any number) of 8 values to a row of T, rounded once.
 template <typename T>
-__device__ __forceinline__ void store8(T *p, int left, bool wide, const float *v) {
-    if (wide && left >= 8) {
-        struct __attribute__((aligned(16))) Eight {
-            T v[8];
-        } e;
+__device__ __forceinline__ void store8(T *p, int left, bool wide, bool stream, const float *v) {
+    struct Eight {
+        T v[8];
+    } e;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            e.v[i] = static_cast<T>(v[i]);
-        *reinterpret_cast<Eight *>(p) = e;
+    for (int i = 0; i < 8; ++i)
+        e.v[i] = static_cast<T>(v[i]);
+    if (wide && left >= 8) {
+        struct Pieces {
+            u4 v[sizeof(T) / 2];
+        };
+        const Pieces pieces = __builtin_bit_cast(Pieces, e);
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+            put(reinterpret_cast<u4 *>(p) + i, pieces.v[i], stream);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < left)
-            p[i] = static_cast<T>(v[i]);
+            p[i] = e.v[i];
+}
+
+// Eight values that are read once, `left` of them there.
+template <typename T>
+__device__ __forceinline__ void read8(const T *p, int left, bool wide, bool stream, float *v) {
+    if (stream && wide && left >= 8) {
+        struct __attribute__((aligned(16))) Pieces {
+            u4 v[sizeof(T) / 2];
+        } pieces;
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+            pieces.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p) + i);
+        load8(reinterpret_cast<const T *>(&pieces), v);
+        return;
+    }
+    load8_tail(p, left, wide, v);
 }
 
 // Eight values of h from column c on.
 template <typename T, typename R>
 __device__ __forceinline__ void load_sum(const NormArgs &a, int32_t row, int32_t c, float *h) {
-    load8_tail(static_cast<const T *>(a.x) + row * a.ldx + c, a.cols - c, a.wide_x, h);
+    read8(static_cast<const T *>(a.x) + row * a.ldx + c, a.cols - c, a.wide_x, a.stream, h);
     if constexpr (!std::is_same_v<R, None>) {
         float r[8];
-        load8_tail(static_cast<const R *>(a.residual) + row * a.ldr + c, a.cols - c, a.wide_r, r);
+        read8(static_cast<const R *>(a.residual) + row * a.ldr + c, a.cols - c, a.wide_r, a.stream, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             h[i] += r[i];
@@ -71,16 +104,16 @@ __device__ __forceinline__ void finish8(const NormArgs &a, int32_t row, int32_t 
                                         float inverse) {
     if constexpr (!std::is_same_v<R, None>)
         if (a.total)
-            store8(static_cast<R *>(a.total) + row * a.ldt + c, a.cols - c, a.wide_t, h);
+            store8(static_cast<R *>(a.total) + row * a.ldt + c, a.cols - c, a.wide_t, a.stream, h);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         v[i] = c + i < a.cols ? h[i] * inverse * g[i] : 0.0f;
     if (a.y) {
         if (a.y32)
-            store8(static_cast<float *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, v);
+            store8(static_cast<float *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, a.stream, v);
         else
-            store8(static_cast<T *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, v);
+            store8(static_cast<T *>(a.y) + row * a.ldy + c, a.cols - c, a.wide_y, a.stream, v);
     }
     if (a.q) {
         uint32_t m = most8(v);
@@ -91,8 +124,8 @@ __device__ __forceinline__ void finish8(const NormArgs &a, int32_t row, int32_t 
         if (b >= a.kb)
             return;
         const Scale s = scale_of(m);
-        *reinterpret_cast<u2 *>(a.q + static_cast<int64_t>(row) * a.kb * kBlock + c) =
-            u2{codes4(v, s.inv), codes4(v + 4, s.inv)};
+        put(reinterpret_cast<u2 *>(a.q + static_cast<int64_t>(row) * a.kb * kBlock + c),
+            u2{codes4(v, s.inv), codes4(v + 4, s.inv)}, a.stream);
         if (c % kBlock == 0)
             a.scale[static_cast<int64_t>(b) * a.rows + row] = s.scale;
     }
@@ -116,20 +149,12 @@ __device__ __forceinline__ float row_sum(float v, float *part) {
     return v;
 }
 
-// The row of this thread: neighbouring rows on one XCD, so that their scales,
-// which lie side by side, leave its L2 as whole lines.
-template <int ROWS>
-__device__ __forceinline__ int32_t own_row(int threads) {
-    const int32_t per = gridDim.x / kXcds, group = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
-    return group * ROWS + threadIdx.x / threads;
-}
-
 // THREADS a row, VECS pieces of 8 values each.
-template <typename T, typename R, typename W, int VECS, int THREADS>
+template <typename T, typename R, typename W, int THREADS, int VECS>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormArgs a) {
     __shared__ float part[16];
-    const int32_t row = own_row<THREADS < 256 ? 256 / THREADS : 1>(THREADS);
-    if (row >= a.rows)
+    const int32_t row = THREADS < 256 ? blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS : blockIdx.x;
+    if (row >= a.rows)  // whole wavefronts, of which each has its own row there
         return;
     const int32_t c0 = threadIdx.x % THREADS * 8;
     float h[VECS][8];
@@ -156,9 +181,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormA
 template <typename T, typename R, typename W>
 __global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
     __shared__ float part[16];
-    const int32_t row = own_row<1>(1024);
-    if (row >= a.rows)
-        return;
+    const int32_t row = blockIdx.x;
     float sum = 0;
     for (int32_t c = threadIdx.x * 8; c < a.cols; c += 8192) {
         float h[8];
@@ -177,22 +200,34 @@ __global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
     }
 }
 
+// Threads a row: as many as there are pieces where rows are few (16 x 4096: 4.0 us, half as many
+// 4.8, a wavefront 10); else two pieces a thread, whose loads are under way together, of rows of a
+// wavefront or more (8192 x 4096 bf16 with residual and codes: 46.3 us, 5.1 TB/s; one piece
+// 48.9, four 53.5; 16384 x 1024 25.3, with 128 threads 27.5; 8192 x 2048 25.4 with one or two).
 template <typename T, typename R, typename W>
 hipError_t launch(const NormArgs &a, hipStream_t stream) {
     const int32_t pieces = (a.cols + 7) / 8;
-    auto grid = [&](int rows) { return ((a.rows + rows - 1) / rows + kXcds - 1) / kXcds * kXcds; };
+    const bool few = a.rows < 512;
     if (pieces <= 64)
-        norm_rows<T, R, W, 1, 64><<<grid(4), 256, 0, stream>>>(a);
+        norm_rows<T, R, W, 64, 1><<<(a.rows + 3) / 4, 256, 0, stream>>>(a);
+    else if (pieces <= 128 && !few)
+        norm_rows<T, R, W, 64, 2><<<(a.rows + 3) / 4, 256, 0, stream>>>(a);
     else if (pieces <= 256)
-        norm_rows<T, R, W, 1, 256><<<grid(1), 256, 0, stream>>>(a);
+        norm_rows<T, R, W, 256, 1><<<a.rows, 256, 0, stream>>>(a);
+    else if (pieces <= 512 && few)
+        norm_rows<T, R, W, 512, 1><<<a.rows, 512, 0, stream>>>(a);
     else if (pieces <= 512)
-        norm_rows<T, R, W, 2, 256><<<grid(1), 256, 0, stream>>>(a);
+        norm_rows<T, R, W, 256, 2><<<a.rows, 256, 0, stream>>>(a);
+    else if (pieces <= 1024 && few)
+        norm_rows<T, R, W, 1024, 1><<<a.rows, 1024, 0, stream>>>(a);
     else if (pieces <= 1024)
-        norm_rows<T, R, W, 4, 256><<<grid(1), 256, 0, stream>>>(a);
+        norm_rows<T, R, W, 512, 2><<<a.rows, 512, 0, stream>>>(a);
+    else if (pieces <= 2048)
+        norm_rows<T, R, W, 1024, 2><<<a.rows, 1024, 0, stream>>>(a);
     else if (pieces <= 4096)
-        norm_rows<T, R, W, 4, 1024><<<grid(1), 1024, 0, stream>>>(a);
+        norm_rows<T, R, W, 1024, 4><<<a.rows, 1024, 0, stream>>>(a);
     else
-        norm_long<T, R, W><<<grid(1), 1024, 0, stream>>>(a);
+        norm_long<T, R, W><<<a.rows, 1024, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -227,6 +262,7 @@ hipError_t launch_norm(NormArgs a, int32_t type, bool residual32, bool gain32, h
     a.wide_t = wide(a.total, a.ldt, of_r);
     a.wide_g = wide(a.gain, 0, 1);
     a.wide_y = wide(a.y, a.ldy, a.y32 ? 4 : size);
+    a.stream = static_cast<int64_t>(a.rows) * a.cols * size >= 16 << 20;
     return type == kF32   ? with_residual<float>(a, residual32, gain32, stream)
            : type == kF16 ? with_residual<_Float16>(a, residual32, gain32, stream)
                           : with_residual<__bf16>(a, residual32, gain32, stream);
