@@ -276,26 +276,41 @@ class Experts:
 class ExpertLayer:
     """A mixture-of-experts layer for one batch size, as a model's forward pass
     runs it: the router's logits (``spconv_linear``, fp32), ``route``, the chosen
-    ``Experts``, the residual sum and, where ``head`` is given, a dense 8-bit
-    layer on top.
+    ``Experts``, the residual sum and, where ``head`` is given, a dense layer in
+    8 or 4 bits (``Fp8Linear``, ``Mxfp4Linear``) on top.
 
     ``router`` is the router's weight [experts, hidden] in float32; ``score``,
-    ``bias``, ``groups``, ... are route()'s.  Buffers are made once; every step is
-    queued on torch's current stream.  ``capture`` records the steps into one
-    graph (torch.cuda.CUDAGraph over HIP graphs) and ``replay`` launches it on
-    what ``x`` holds.
+    ``bias``, ``groups``, ... are route()'s.  ``norm`` and ``head_norm`` are gains
+    [hidden]: with the one the router and the experts read rms_norm(x) with
+    ``eps`` (the residual stays x), with the other the head reads the sum's, which
+    an ``Fp8Linear`` takes as the norm's own codes.  ``sampler``, a dict of
+    sample()'s temperature, top_k, top_p and min_p, ends the step with the
+    choice of ``tokens`` [batch] from the output as logits and the random numbers
+    in ``u`` [batch].  Buffers are made once; every step is queued on torch's
+    current stream.  ``capture`` records the steps into one graph
+    (torch.cuda.CUDAGraph over HIP graphs) and ``replay`` launches it on what
+    ``x`` and ``u`` hold.
     """
 
-    def __init__(self, router, experts: Experts, k: int, batch: int, dtype=None, head: Fp8Linear = None,
+    def __init__(self, router, experts: Experts, k: int, batch: int, dtype=None, head=None,
                  residual: bool = True, score: str = "softmax", bias=None, groups: int = 1, groups_kept: int = 1,
-                 group_top: int = 1, renorm: bool = True, factor: float = 1.0):
+                 group_top: int = 1, renorm: bool = True, factor: float = 1.0, norm=None, head_norm=None,
+                 eps: float = 1e-6, sampler: dict = None):
         import torch
+
+        from . import serving
         dev, f32 = experts.w13.device, torch.float32
         dtype = dtype or torch.bfloat16
         _type(dtype, "dtype")
         self.router = _given(router, (experts.experts, experts.hidden), f32, dev, "router")
         if head is not None and head.cin != experts.hidden:
             raise ValueError("head must take %d channels" % experts.hidden)
+        if head is None and head_norm is not None:
+            raise ValueError("head_norm needs a head")
+        for gain, what in ((norm, "norm"), (head_norm, "head_norm")):
+            if gain is not None:
+                _given(gain, (experts.hidden,), f32 if gain.dtype != dtype else dtype, dev, what)
+        self.serving, self.norm, self.head_norm, self.eps, self.sampler = serving, norm, head_norm, float(eps), sampler
         self.experts, self.head, self.k, self.residual = experts, head, int(k), residual
         self.choice = dict(score=score, bias=bias, groups=groups, groups_kept=groups_kept, group_top=group_top,
                            renorm=renorm, factor=factor)
@@ -312,6 +327,18 @@ class ExpertLayer:
         self.space = torch.empty(experts.workspace_bytes(batch, k), dtype=torch.uint8, device=dev)
         self.head_space = None if head is None else torch.empty(head.workspace_bytes(batch, dtype), dtype=torch.uint8,
                                                                 device=dev)
+        self.h = self.x if norm is None else make(experts.hidden, dtype)
+        # the head's input: rows, or with a norm before an 8-bit head its codes and scales
+        self.top = self.y if head_norm is None else None if isinstance(head, Fp8Linear) else make(experts.hidden, dtype)
+        if self.top is None and head is not None:
+            kb = _blocks(experts.hidden)
+            self.q = torch.zeros((batch, kb * BLOCK), dtype=torch.float8_e4m3fn, device=dev)
+            self.q_scale = torch.zeros((kb, batch), dtype=f32, device=dev)
+        if sampler is not None:
+            self.u, self.tokens = torch.zeros(batch, dtype=f32, device=dev), torch.zeros(batch, dtype=torch.int32, device=dev)
+            self.sample_space = torch.empty(
+                max(serving.spconv_sample_workspace(_type(dtype, "dtype"), batch, self.out.shape[1]), 1),
+                dtype=torch.uint8, device=dev)
         self.graph = None
 
     def forward(self, x=None):
@@ -319,15 +346,34 @@ class ExpertLayer:
         if x is not None:
             self.x.copy_(x)
         e = self.experts
-        self.x32.copy_(self.x)
+        if self.norm is None:
+            self.x32.copy_(self.x)
+        else:
+            self.serving.rms_norm(self.x, self.norm, self.eps, y=self.x32)
+            self.h.copy_(self.x32)
         spconv_linear(self.x32, self.router, None, "none", self.logits, self.x.shape[0], e.hidden, e.experts)
         route(self.logits, self.k, ids=self.ids, weights=self.weights, **self.choice)
-        e.run(self.x, self.ids, self.weights, self.y, self.space)
-        if self.residual:
-            self.y.add_(self.x)
-        if self.head is not None:
-            self.head.run(self.y, y=self.out, workspace=self.head_space)
+        e.run(self.h, self.ids, self.weights, self.y, self.space)
+        if self.head_norm is not None:
+            self._normed_head()
+        else:
+            if self.residual:
+                self.y.add_(self.x)
+            if self.head is not None:
+                self.head.run(self.y, y=self.out, workspace=self.head_space)
+        if self.sampler is not None:
+            self.serving.sample(self.out, self.u, ids=self.tokens, workspace=self.sample_space, **self.sampler)
         return self.out
+
+    def _normed_head(self):
+        """The residual sum (into y), its norm and the head: the sum and the norm are one pass over the rows."""
+        x, total = (self.x, self.y) if self.residual else (self.y, None)
+        if self.top is None:
+            self.serving.rms_norm_fp8(x, self.head_norm, self.eps, total, q=self.q, scale=self.q_scale, total=total)
+            self.head.run(self.q, self.q_scale, y=self.out, workspace=self.head_space)
+        else:
+            self.serving.rms_norm(x, self.head_norm, self.eps, total, y=self.top, total=total)
+            self.head.run(self.top, y=self.out, workspace=self.head_space)
 
     def capture(self):
         """Record the steps into one graph (after one warm-up pass)."""
