@@ -430,8 +430,9 @@ SPCONV_API spconv_status spconv_linear_mxfp4_workspace(spconv_dtype x_dtype, int
  *   total = h, rounded once
  *   v     = h / sqrt( sum h^2 / cols + eps ) * gain   (gain 1 where NULL)
  *   y     = v, rounded once;  q, scale = v as by spconv_quantize_fp8 with block_rows = 1
- * all in fp32: the norm is that of h before it is rounded, codes are those of v
- * in fp32.  Squares are fp32, too: a row whose sum of squares passes 2^128 gives zeros.
+ * in fp32, the sum's last additions and the root in fp64: the norm is that of h before
+ * it is rounded, codes are those of v in fp32.  Squares are fp32, too: a row in which one, or
+ * the sum over a thread's few channels, passes 2^128 gives zeros.
  *   x         device, [rows][cols] of dtype (F32, F16 or BF16), row stride ldx >= cols elements
  *   residual  device, of residual_dtype with row stride ldr, or NULL
  *   total     out, of residual_dtype with row stride ldt, or NULL

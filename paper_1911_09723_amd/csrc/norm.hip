@@ -3,9 +3,13 @@
 //
 //     h = x + r,  total = h rounded to r's type,  y = h * (1 / sqrt(sum h^2 / cols + eps)) * gain,
 //
-// all in 32 bits; y is rounded once to its type, or quantised by blocks of 128
-// channels as quantize_fp8's rows are (fp8.hpp).  The norm is that of the
-// 32-bit h, not of the rounded total: one rounding less between x and y.
+// in 32 bits but for what a row's threads found and the root, which are joined and taken in 64: a
+// factor of all of a row is off by its rounding alone, and y by 4.3e-8 of it on average (5.5e-8
+// with 32 bits there, 2048 columns; the time is the same.  With the products in 64 bits, or each
+// with its rounding's error carried on, 3.6e-8, and 8192 x 4096 takes 28.0 to 32.6 and 30.3 us).  y
+// is rounded once to its type, or quantised by blocks of 128 channels as quantize_fp8's rows are
+// (fp8.hpp).  The norm is that of the 32-bit h, not of the rounded total: one rounding less
+// between x and y.
 //
 // One pass: a row stays in registers between its sum of squares and its
 // results, 8 neighbouring values a thread and piece, so that 16 lanes hold a
@@ -133,7 +137,7 @@ __device__ __forceinline__ void finish8(const NormArgs &a, int32_t row, int32_t 
 
 // The sum over a row's THREADS threads, in a fixed order.
 template <int THREADS>
-__device__ __forceinline__ float row_sum(float v, float *part) {
+__device__ __forceinline__ double row_sum(double v, double *part) {
 #pragma unroll
     for (int s = 1; s < 64; s *= 2)
         v += __shfl_xor(v, s);
@@ -149,10 +153,23 @@ __device__ __forceinline__ float row_sum(float v, float *part) {
     return v;
 }
 
+__device__ __forceinline__ float add_squares(const float *h, float sum) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        sum = fmaf(h[i], h[i], sum);
+    return sum;
+}
+
+// 1 / sqrt(sum / cols + eps): the instruction's 2^-25 or so, and one step of Newton's.
+__device__ __forceinline__ float inverse_of(const NormArgs &a, double sum) {
+    const double mean = fma(sum, a.share, static_cast<double>(a.eps)), r = __builtin_amdgcn_rsq(mean);
+    return static_cast<float>(mean > 0 && mean < INFINITY ? fma(0.5 * r, fma(-mean * r, r, 1.0), r) : r);
+}
+
 // THREADS a row, VECS pieces of 8 values each.
 template <typename T, typename R, typename W, int THREADS, int VECS>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormArgs a) {
-    __shared__ float part[16];
+    __shared__ double part[16];
     const int32_t row = THREADS < 256 ? blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS : blockIdx.x;
     if (row >= a.rows)  // whole wavefronts, of which each has its own row there
         return;
@@ -164,10 +181,8 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormA
     float sum = 0;
 #pragma unroll
     for (int u = 0; u < VECS; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            sum = fmaf(h[u][i], h[u][i], sum);
-    const float inverse = 1.0f / sqrtf(row_sum<THREADS>(sum, part) / static_cast<float>(a.cols) + a.eps);
+        sum = add_squares(h[u], sum);
+    const float inverse = inverse_of(a, row_sum<THREADS>(sum, part));
 #pragma unroll
     for (int u = 0; u < VECS; ++u) {
         float g[8];
@@ -180,17 +195,15 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormA
 // before it writes it, so total and y may lie where residual and x do.
 template <typename T, typename R, typename W>
 __global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
-    __shared__ float part[16];
+    __shared__ double part[16];
     const int32_t row = blockIdx.x;
     float sum = 0;
     for (int32_t c = threadIdx.x * 8; c < a.cols; c += 8192) {
         float h[8];
         load_sum<T, R>(a, row, c, h);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            sum = fmaf(h[i], h[i], sum);
+        sum = add_squares(h, sum);
     }
-    const float inverse = 1.0f / sqrtf(row_sum<1024>(sum, part) / static_cast<float>(a.cols) + a.eps);
+    const float inverse = inverse_of(a, row_sum<1024>(sum, part));
     for (int32_t c0 = 0; c0 < a.cols; c0 += 8192) {  // whole wavefronts: blocks are found across lanes
         const int32_t c = c0 + threadIdx.x * 8;
         float h[8], g[8];
@@ -262,6 +275,7 @@ hipError_t launch_norm(NormArgs a, int32_t type, bool residual32, bool gain32, h
     a.wide_t = wide(a.total, a.ldt, of_r);
     a.wide_g = wide(a.gain, 0, 1);
     a.wide_y = wide(a.y, a.ldy, a.y32 ? 4 : size);
+    a.share = 1.0 / a.cols;
     a.stream = static_cast<int64_t>(a.rows) * a.cols * size >= 16 << 20;
     return type == kF32   ? with_residual<float>(a, residual32, gain32, stream)
            : type == kF16 ? with_residual<_Float16>(a, residual32, gain32, stream)

@@ -24,7 +24,8 @@ struct NormArgs {
     bool y32;                         // y in f32, else in x's type
     // set by launch_norm: rows that can be read and written in pieces of 16 bytes, and how
     bool wide_x, wide_r, wide_g, wide_t, wide_y;
-    bool stream;  // past the caches
+    bool stream;   // past the caches
+    double share;  // 1 / cols
 };
 // type: of x; residual and gain are of that type or (residual32, gain32) in f32.
 hipError_t launch_norm(NormArgs a, int32_t type, bool residual32, bool gain32, hipStream_t stream);

@@ -187,6 +187,8 @@ class Mxfp4Linear:
 def _column(p, n: int, dtype, device, what: str):
     """(address, value) of a parameter: a tensor with a value for each row, or a number for all."""
     if isinstance(p, (int, float)):
+        if dtype is _experts._torch.int32 and not -2 ** 31 <= p < 2 ** 31:
+            raise ValueError("%s must be a number of 32 bits" % what)
         return None, p
     if p.dtype != dtype or p.dim() != 1 or p.shape[0] != n or p.get_device() != device or not p.is_contiguous():
         raise ValueError("%s must be a number or a contiguous %s tensor of %d values on GPU %d" % (what, dtype, n, device))

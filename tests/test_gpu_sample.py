@@ -92,6 +92,20 @@ def test_parameters_out_of_their_ranges():
     assert sp.sample(logits, u, t, k, p, m)[9].item() == logits[9].argmax().item()
 
 
+@pytest.mark.parametrize("vocab", [1000, 40000])
+def test_temperatures_of_every_size(vocab):
+    """From the smallest float, where the largest logit takes all, to infinity, where tokens weigh the same."""
+    import torch
+    each = [1e-45, 1e-38, 1e-10, 1e-3, 30.0, 1e10, 3e38, INF]
+    logits, u = _logits(8, vocab, "f32", 21), _u(8, 22)
+    logits[:, 7] = 3e38 if vocab > 20000 else 5.0
+    for f in (dict(), dict(top_k=30), dict(top_p=0.9), dict(min_p=0.5), dict(top_k=600)):
+        note("temperatures %d %s" % (vocab, f))
+        _compare(logits, u, _given(each, torch.float32), f.get("top_k", 0), f.get("top_p", 1.0), f.get("min_p", 0.0))
+        for t in each:
+            _compare(logits[:2], u[:2], t, **f)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [1000, 40000])
 def test_masked_tokens(vocab, dtype):
@@ -209,7 +223,7 @@ def test_no_rows_and_refusals():
     for call in (lambda: sp.sample(x, 0.5), lambda: sp.sample(x, u[:2]), lambda: sp.sample(x, u.cpu()),
                  lambda: sp.sample(x, u.double()), lambda: sp.sample(x[0], u), lambda: sp.sample(x[:, ::2], u),
                  lambda: sp.sample(x, u, u[:2]), lambda: sp.sample(x, u, top_k=u), lambda: sp.sample(x, u, top_p=u.half()),
-                 lambda: sp.sample(x, u, ids=u), lambda: sp.sample(x, u, min_p=torch.zeros((3, 1), device=device()))):
+                 lambda: sp.sample(x, u, ids=u), lambda: sp.sample(x, u, top_k=(1 << 32) + 5), lambda: sp.sample(x, u, min_p=torch.zeros((3, 1), device=device()))):
         with pytest.raises(ValueError):
             call()
     for f in (dict(temperature=-1.0), dict(top_k=-1), dict(top_p=1.1), dict(min_p=-0.5), dict(temperature=float("nan"))):
