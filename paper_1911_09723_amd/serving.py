@@ -25,9 +25,10 @@ def _lines(n: int) -> int:
     return -(-n // LINE)
 
 
-def _rows_like(t, rows: int, cols: int, device, what: str) -> int:
-    """The row stride of t, checked to be rows x cols with contiguous rows on this device."""
-    if t.get_device() != device or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+def _rows_like(t, shape, device, what: str) -> int:
+    """The row stride of t, checked to be a matrix of this shape with contiguous rows on this device."""
+    rows, cols = shape
+    if t.shape != shape or t.get_device() != device:
         raise ValueError("%s must be a matrix [%d, %d] on GPU %d" % (what, rows, cols, device))
     ld, step = t.stride()
     if (step != 1 and cols > 1) or (rows > 1 and ld < cols):
@@ -39,24 +40,25 @@ def _norm(x, gain, eps, residual, total, y, q, scale, stream):
     """Queue the norm of x into the outputs given; returns total (made here where a residual is given)."""
     kind = _type(x.dtype, "x")
     rows, cols, ldx, device = _matrix(x, "x")
+    shape = rows, cols
     kind_r = kind_g = kind_y = F32
     at_r = at_t = at_g = at_y = None
     ldr = ldt = ldy = 0
     if residual is not None:
-        ldr, kind_r, at_r = _rows_like(residual, rows, cols, device, "residual"), _type(residual.dtype, "residual"), residual.data_ptr()
+        ldr, kind_r, at_r = _rows_like(residual, shape, device, "residual"), _type(residual.dtype, "residual"), residual.data_ptr()
         if total is None:
-            total = residual.new_empty((rows, cols))
+            total = _experts._torch.empty_like(residual)  # a fraction of a microsecond less than new_empty
         elif total.dtype != residual.dtype:
             raise ValueError("total must have the residual's type")
-        ldt, at_t = _rows_like(total, rows, cols, device, "total"), total.data_ptr()
+        ldt, at_t = _rows_like(total, shape, device, "total"), total.data_ptr()
     elif total is not None:
         raise ValueError("total is the sum with a residual")
     if gain is not None:
         kind_g, at_g = _type(gain.dtype, "gain"), gain.data_ptr()
-        if gain.dim() != 1 or gain.shape[0] != cols or gain.get_device() != device or not gain.is_contiguous():
+        if gain.shape != (cols,) or gain.get_device() != device or not gain.is_contiguous():
             raise ValueError("gain must be a contiguous vector of %d values on GPU %d" % (cols, device))
     if y is not None:
-        ldy, kind_y, at_y = _rows_like(y, rows, cols, device, "y"), _type(y.dtype, "y"), y.data_ptr()
+        ldy, kind_y, at_y = _rows_like(y, shape, device, "y"), _type(y.dtype, "y"), y.data_ptr()
     if rows and cols:
         _check(_experts._lib.spconv_rms_norm(
             x.data_ptr(), kind, ldx, at_r, kind_r, ldr, at_t, ldt, at_g, kind_g, eps, at_y, kind_y, ldy,
@@ -70,8 +72,9 @@ def rms_norm(x, gain=None, eps: float = 1e-6, residual=None, y=None, dtype=None,
     (or x): a matrix [rows, cols] of ``dtype`` (x's, or float32).  With a residual
     the pair (y, total): total is h in the residual's type, into ``total`` (a new
     tensor, or the residual itself) where given."""
+    _type(x.dtype, "x")
     if y is None:
-        y = x.new_empty(x.shape, dtype=dtype)
+        y = _experts._torch.empty_like(x, dtype=dtype) if dtype else _experts._torch.empty_like(x)
     elif dtype is not None and y.dtype != dtype:
         raise ValueError("y must be of dtype")
     total = _norm(x, gain, eps, residual, total, y, None, None, stream)
@@ -190,7 +193,7 @@ def _column(p, n: int, dtype, device, what: str):
         if dtype is _experts._torch.int32 and not -2 ** 31 <= p < 2 ** 31:
             raise ValueError("%s must be a number of 32 bits" % what)
         return None, p
-    if p.dtype != dtype or p.dim() != 1 or p.shape[0] != n or p.get_device() != device or not p.is_contiguous():
+    if p.dtype != dtype or p.shape != (n,) or p.get_device() != device or not p.is_contiguous():
         raise ValueError("%s must be a number or a contiguous %s tensor of %d values on GPU %d" % (what, dtype, n, device))
     return p.data_ptr(), 0
 
