@@ -106,6 +106,21 @@ def test_temperatures_of_every_size(vocab):
             _compare(logits[:2], u[:2], t, **f)
 
 
+@pytest.mark.parametrize("vocab", [1000, 40000])
+def test_distances_past_the_largest_float(vocab):
+    """Logits of both ends of float32: their distance is infinite there, and they weigh the same where t is."""
+    logits = _logits(6, vocab, "f32", 31)
+    logits[:, 5:vocab // 2] = -3e38
+    logits[:, vocab - 7] = 3e38
+    logits[2:4, 9:90] = -INF
+    u = _u(6, 32)
+    for t in (INF, 3e38, 1e37, 1.0):
+        for f in (dict(), dict(top_k=vocab // 4), dict(top_k=vocab - 3), dict(top_p=0.3), dict(top_p=0.999999), dict(min_p=0.5),
+                  dict(top_k=vocab - 100, top_p=0.9)):
+            note("distances %d t = %g %s" % (vocab, t, f))
+            _compare(logits, u, t, **f)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [1000, 40000])
 def test_masked_tokens(vocab, dtype):
