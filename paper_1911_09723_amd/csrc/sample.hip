@@ -37,11 +37,13 @@
 // walks over the whole row.
 //
 // What bounds it.  64 x 131072 in bf16 (16.8 MB, 3.3 us at a copy's rate), on the device alone: t = 0
-// 8.8 us; no filter 23, of it 9 the exponentials (25 64-bit operations each); k = 50 20, of it 13
-// the steps of B, one after the other, each some loads or a few LDS accesses and barriers long; p =
-// 0.9 63: A 7, B 17.5 (exponentials and LDS atomics), C 18.5, D 19.7.  One row of 4000: 8.4 to
-// 9.1, with p 14.6.  Steps one after the other are why a workgroup has 512 threads and not 1024
-// (each thread's share of such a step is done by twice as many: k = 50 of 4000 took 14 us).
+// 8.8 us; no filter 23, of it 9 the exponentials (25 64-bit operations each); k = 50 20, of it 10
+// the steps of B, one after the other, each some loads or a few LDS accesses and barriers long (1000
+// to 2500 cycles; k = 500 24); p = 0.9 56: A 6.5, B 16.7 (exponentials and LDS atomics), C 12.9, D
+// 19.7 (the border in 1200 listed tokens 9, the token 5).  One row of 4000: 8.4 to 9.1, with p 13.3.
+// Steps one after the other are why a workgroup has 512 threads and not 1024 (each thread's share
+// of such a step is done by twice as many: k = 50 of 4000 took 14 us).  They wait for their own
+// results, not for instructions: the same steps done again at once take nine tenths.
 #include <algorithm>
 
 #include "fp8.hpp"
@@ -991,18 +993,22 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
             k[j] = g0 + t + j * kThreads < segments ? s.segments[g0 + t + j * kThreads] : 0;
     };
     eight(0, head);
-    auto keys = [&](auto f) {  // f(key, segment) by all threads as often
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            f(head[j], t + j * kThreads);
+    auto eights = [&](auto f) {  // f(eight keys, the first one's segment) by all threads as often; kThreads from one to the next
+        f(head, t);
 #pragma unroll 1
         for (int32_t g0 = kThreads * 8; g0 < segments; g0 += kThreads * 8) {
             uint64_t k[8];
             eight(g0, k);
+            f(k, g0 + t);
+        }
+    };
+    auto keys = [&](auto f) {  // f(key) for every segment that has a token
+        eights([&](const uint64_t (&k)[8], int32_t) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                f(k[j], g0 + t + j * kThreads);
-        }
+                if (k[j])
+                    f(k[j]);
+        });
     };
     const uint64_t best = best_of(s, chunks);
     if (best == 0) {
@@ -1012,10 +1018,7 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
     }
     const float most = logit_of(best);
     clear(sh.bins, kBins);
-    keys([&](uint64_t k, int32_t) {
-        if (k)
-            atomicAdd(&sh.bins[bin_of(logit_of(k), most)], Sum(1));
-    });
+    keys([&](uint64_t k) { atomicAdd(&sh.bins[bin_of(logit_of(k), most)], Sum(1)); });
     __syncthreads();
     const Found f = find(sh, sh.bins, r.top_k, 1.0);
     uint64_t least = 0;  // with fewer segments that have a token than k
@@ -1023,28 +1026,34 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
     if (f.bin >= 0 && f.upto > kFew) {  // more than 1024 up to the end of that bin
         bin = -1;
         least = least_key(sh, r.top_k, 0, 32 + kIndexBits, kFew, [&](auto g) {
-            keys([&](uint64_t k, int32_t) {
-                if (k)
-                    g(k, Sum(1));
-            });
+            keys([&](uint64_t k) { g(k, Sum(1)); });
         });
     }
+    // whether a token that is on, or a segment's largest, is above the bound: by its distance's bits, as bin_of
+    uint32_t end = end_of(bin);
+    auto in_bound = [&](uint64_t key, float l) {
+        return __float_as_uint(most - l) < end && (least == 0 || key >= least);
+    };
     uint32_t *ids = sh.rank;  // (until the list is sorted)
     if (threadIdx.x == 0)
         sh.count = 0;
     __syncthreads();
-    keys([&](uint64_t k, int32_t g) {
-        const bool in = k && k >= least && bin_of(logit_of(k), most) >= bin;
-        if (__any(in)) {
-            const uint32_t at = place_in(&sh.count, in);
-            if (in)
-                ids[at] = g;
-        }
+    eights([&](const uint64_t (&k)[8], int32_t g) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            hits |= static_cast<uint32_t>(k[j] && in_bound(k[j], logit_of(k[j]))) << j;
+        uint32_t at = place_in(&sh.count, __popc(hits));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (hits >> j & 1)
+                ids[at++] = g + j * kThreads;
     });
     __syncthreads();
     const int32_t few = static_cast<int32_t>(sh.count);
-    // f(eight logits, their first token) for the pieces of these segments, all threads as often, four
-    // loads under way at once
+    // f(logits, first tokens) for four pieces of 8 of these segments at once, all threads as often: their
+    // loads are under way together, and one place in the list is asked for (64 x 131072, k = 500: 27.1 us
+    // with a place for each piece and for each of a thread's segments)
     auto walk = [&](auto f) {
 #pragma unroll 1
         for (int32_t q = 0; q < few * 4; q += kThreads * 4) {
@@ -1057,18 +1066,15 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
                 at[p] = g / kSegments * kChunk + (e & 3) * 2048 + g % kSegments * 8;
                 load_logits(static_cast<const T *>(a.logits) + row * a.ld + at[p], e < few * 4 ? a.vocab - at[p] : 0, v[p]);
             }
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-                if (q + p * kThreads < few * 4)
-                    f(v[p], at[p]);
+            f(v, at, few * 4 - q);
         }
     };
     auto every = [&](auto f) {
-        walk([&](const float *v, int32_t i) {
+        walk([&](const float (&v)[4][8], const int32_t (&at)[4], int32_t) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (v[j] > -INFINITY)
-                    f(v[j], i + j);
+            for (int j = 0; j < 32; ++j)
+                if (v[j / 8][j % 8] > -INFINITY)
+                    f(v[j / 8][j % 8], at[j / 8] + j % 8);
         });
     };
     auto list = [&] {
@@ -1076,18 +1082,26 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
         if (threadIdx.x == 0)
             sh.count = 0;
         __syncthreads();
-        walk([&](const float *v, int32_t i) {
+        walk([&](const float (&v)[4][8], const int32_t (&at)[4], int32_t left) {
             uint32_t hits = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                hits |= static_cast<uint32_t>(v[j] > -INFINITY && key_of(v[j], i + j) >= least && bin_of(v[j], most) >= bin) << j;
-            uint32_t at = place_in(&sh.count, __popc(hits));
+            for (int p = 0; p < 4; ++p)
+                if (p * kThreads < left) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (hits >> j & 1) {
-                    if (at < kFew)
-                        sh.few[at] = key_of(v[j], i + j);
-                    ++at;
+                    for (int j = 0; j < 8; ++j)
+                        hits |= static_cast<uint32_t>(v[p][j] > -INFINITY && in_bound(key_of(v[p][j], at[p] + j), v[p][j])) << (p * 8 + j);
+                }
+            uint32_t to = place_in(&sh.count, __popc(hits));
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                if (p * kThreads < left) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (hits >> (p * 8 + j) & 1) {
+                            if (to < kFew)
+                                sh.few[to] = key_of(v[p][j], at[p] + j);
+                            ++to;
+                        }
                 }
         });
         __syncthreads();
@@ -1101,9 +1115,8 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
         });
         __syncthreads();
         const Found t = find(sh, sh.bins, r.top_k, 1.0);
-        bin = t.bin;
+        end = end_of(t.upto > kFew ? -1 : t.bin);
         if (t.upto > kFew) {
-            bin = -1;
             least = least_key(sh, r.top_k, 0, 32 + kIndexBits, kFew, [&](auto g) {
                 every([&](float v, int32_t i) { g(key_of(v, i), Sum(1)); });
             });
@@ -1113,9 +1126,10 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
     pick_few(a, row, r, static_cast<int32_t>(sh.count), most, sh);
 }
 
-// B
+// B.  Six wavefronts a SIMD are three workgroups a compute unit: with the 97 registers that it would take
+// there are two (64 x 131072 with parameters by row 36.7 us and 32.1; with 64 registers 36.8).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_rows(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 6) sample_rows(SampleArgs a) {
     __shared__ Shared sh;
     const int32_t row = blockIdx.y, chunk = blockIdx.x, chunks = chunks_of(a.vocab);  // (one workgroup where it does all)
     const Row r = row_of(a, row);
