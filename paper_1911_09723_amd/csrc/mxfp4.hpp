@@ -54,13 +54,22 @@ struct Eight {
 typedef uint16_t us2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bh2 __attribute__((ext_vector_type(2)));
 
-// Eight neighbours from p, of which `left` exist; the others are zeros.
-template <typename T>
+// Eight neighbours from p, of which `left` exist; the others are zeros.  STREAM: past the caches.
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ Eight<T> eight_tail(const T *p, int left, bool wide) {
     struct __attribute__((aligned(16))) Piece {
         T v[8];
     };
     Eight<T> r;
+    if (STREAM && wide && left >= 8) {
+        struct Pieces {
+            u4 v[sizeof(T) / 2];
+        } a;
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+            a.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p) + i);
+        return __builtin_bit_cast(Eight<T>, a);
+    }
     if (wide && left >= 8) {
         const Piece a = *reinterpret_cast<const Piece *>(p);
 #pragma unroll

@@ -866,14 +866,14 @@ __global__ void __launch_bounds__(kSegments) sample_chunks(SampleArgs a) {
     if (best) {
         const float most = logit_of(best);
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {  // from the first-level cache: a loop over registers would have to be unrolled
-            const int32_t i = chunk * kChunk + j * 2048 + static_cast<int32_t>(threadIdx.x) * 8;
-            float w[8];
-            load_logits(l + i, a.vocab - i, w);
+        for (int j = 0; j < 4; ++j) {  // moves, as registers take no index (read again 25.6 us in place of 23.5, 256 x 50001)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const Sum u = units(weight_of(w[e], most, r), r);
-                sum += w[e] > -INFINITY ? u : 0;
+                const Sum u = units(weight_of(v[0][e], most, r), r);
+                sum += v[0][e] > -INFINITY ? u : 0;
+                v[0][e] = v[1][e];
+                v[1][e] = v[2][e];
+                v[2][e] = v[3][e];
             }
         }
     }
