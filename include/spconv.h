@@ -379,8 +379,9 @@ SPCONV_API spconv_status spconv_linear_fp8_workspace(spconv_dtype x_dtype, int32
  *   q, scale  out, in the form above
  * rows == 0 or cols == 0 is a no-op.
  * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
- * cols, bad dtype or alignment, overlap), SPCONV_E_SHAPE (rows * ceil(cols /
- * 256) of 2^28 or more, cols above 2^30, ldx above 2^34), SPCONV_E_HIP.
+ * cols, bad dtype or alignment, overlap), SPCONV_E_SHAPE (rows of 2^25 or more,
+ * rows * ceil(cols / 256) of 2^28 or more, cols above 2^30, ldx above 2^34),
+ * SPCONV_E_HIP.
  */
 SPCONV_API spconv_status spconv_quantize_mxfp4(const void *x, spconv_dtype dtype, int64_t ldx, int32_t rows,
                                                int32_t cols, void *q, void *scale, void *stream);
@@ -405,8 +406,8 @@ SPCONV_API spconv_status spconv_quantize_mxfp4(const void *x, spconv_dtype dtype
  * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, ldx <
  * cin, bad dtype, act or alignment, x_scale missing or not asked for, workspace
  * too small, overlap), SPCONV_E_SHAPE (cin == 0 with outputs, cin or cout above
- * 2^22, n * ceil(cin / 256) of 2^27 or more, cout * ceil(cin / 256) of 2^28 or
- * more, n * cout of 2^36 or more, ldx above 2^34), SPCONV_E_HIP.
+ * 2^22, n of 2^25 or more, n * ceil(cin / 256) of 2^27 or more, cout * ceil(cin /
+ * 256) of 2^28 or more, n * cout of 2^36 or more, ldx above 2^34), SPCONV_E_HIP.
  */
 SPCONV_API spconv_status spconv_linear_mxfp4(const void *x, spconv_dtype x_dtype, int64_t ldx, const void *x_scale,
                                              const void *w, const void *w_scale, const float *bias, spconv_act act,
@@ -449,8 +450,8 @@ SPCONV_API spconv_status spconv_linear_mxfp4_workspace(spconv_dtype x_dtype, int
  * Errors: SPCONV_E_ARG (NULL pointer with work to do, negative size, a stride
  * below cols, bad dtype or alignment, eps negative, infinite or NaN, total
  * without residual, overlap), SPCONV_E_UNSUPPORTED (a type that is neither dtype
- * nor F32), SPCONV_E_SHAPE (rows * ceil(cols / 128) of 2^27 or more, cols above
- * 2^30, a stride above 2^34), SPCONV_E_HIP.
+ * nor F32), SPCONV_E_SHAPE (rows of 2^25 or more, rows * ceil(cols / 128) of 2^27
+ * or more, cols above 2^30, a stride above 2^34), SPCONV_E_HIP.
  */
 SPCONV_API spconv_status spconv_rms_norm(const void *x, spconv_dtype dtype, int64_t ldx, const void *residual,
                                          spconv_dtype residual_dtype, int64_t ldr, void *total, int64_t ldt,

@@ -14,7 +14,7 @@
 // One pass: a row stays in registers between its sum of squares and its
 // results, 8 neighbouring values a thread and piece, so that 16 lanes hold a
 // block of 128.  What bounds it is traffic, below some MB the launch and one wait for
-// the row's loads (1 x 1280: 3.9 us).
+// the row's loads (1 x 1280: 2.9 us).
 #include <type_traits>
 
 #include "fp8.hpp"
@@ -214,9 +214,9 @@ __global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
 }
 
 // Threads a row: as many as there are pieces where rows are few (16 x 4096: 4.0 us, half as many
-// 4.8, a wavefront 10); else two pieces a thread, whose loads are under way together, of rows of a
-// wavefront or more (8192 x 4096 bf16 with residual and codes: 46.3 us, 5.1 TB/s; one piece
-// 48.9, four 53.5; 16384 x 1024 25.3, with 128 threads 27.5; 8192 x 2048 25.4 with one or two).
+// 4.8); else two pieces a thread, whose loads are under way together (bf16 with residual and codes:
+// 8192 x 4096 46.3 us, 5.1 TB/s, one piece 48.9, four 53.5; 8192 x 2048 25.4 with one or two; 4096
+// x 8192 45.8, one piece 49.8).
 template <typename T, typename R, typename W>
 hipError_t launch(const NormArgs &a, hipStream_t stream) {
     const int32_t pieces = (a.cols + 7) / 8;

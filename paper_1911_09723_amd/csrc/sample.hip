@@ -1351,7 +1351,7 @@ hipError_t launch(const SampleArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-int64_t sample_workspace(int32_t, int32_t n, int32_t vocab) {
+int64_t sample_workspace(int32_t n, int32_t vocab) {
     return chunks_of(vocab) == 1 ? 0 : n * row_words(vocab) * 8;
 }
 

@@ -24,7 +24,8 @@ using spconv::set_error;
 using spconv::size_of;
 using spconv::span;
 
-constexpr int64_t kMostBlocks = int64_t(1) << 27;  // row blocks of a matrix: launches stay below 2^32 threads
+constexpr int64_t kMostBlocks = int64_t(1) << 27;  // row blocks of a matrix and
+constexpr int32_t kMostRows = 1 << 25;             // its rows: launches stay below 2^32 threads
 constexpr int64_t kMostLines = int64_t(1) << 28;   // lines of a weight: their scales lie within 32-bit offsets
 constexpr int64_t kMostOutputs = int64_t(1) << 36;
 constexpr int32_t kMostChannels = 1 << 22;         // a tile of 256 rows lies within 32-bit offsets
@@ -48,8 +49,8 @@ spconv_status check_linear(spconv_dtype x_dtype, int32_t n, int32_t cin, int32_t
         return set_error(SPCONV_E_SHAPE, "cin must be >= 1");
     if (cin > kMostChannels || cout > kMostChannels)
         return set_error(SPCONV_E_SHAPE, "cin and cout must be at most 2^22");
-    if (static_cast<int64_t>(n) * lines_of(cin) >= kMostBlocks)
-        return set_error(SPCONV_E_SHAPE, "n * ceil(cin / 256) must be below 2^27");
+    if (n >= kMostRows || static_cast<int64_t>(n) * lines_of(cin) >= kMostBlocks)
+        return set_error(SPCONV_E_SHAPE, "n must be below 2^25, n * ceil(cin / 256) below 2^27");
     if (static_cast<int64_t>(cout) * lines_of(cin) >= kMostLines)
         return set_error(SPCONV_E_SHAPE, "cout * ceil(cin / 256) must be below 2^28");
     if (static_cast<int64_t>(n) * cout >= kMostOutputs)
@@ -105,9 +106,9 @@ spconv_status spconv_rms_norm(const void *x, spconv_dtype dtype, int64_t ldx, co
         return set_error(SPCONV_E_ARG, "total is the sum with a residual");
     if (ldx < cols || (residual && ldr < cols) || (total && ldt < cols) || (y && ldy < cols))
         return set_error(SPCONV_E_ARG, "row strides must be at least cols");
-    if (cols > (1 << 30) || rows * static_cast<int64_t>(blocks_of(cols)) >= kMostBlocks || ldx > kMostStride ||
+    if (cols > (1 << 30) || rows >= kMostRows || rows * static_cast<int64_t>(blocks_of(cols)) >= kMostBlocks || ldx > kMostStride ||
         (residual && ldr > kMostStride) || (total && ldt > kMostStride) || (y && ldy > kMostStride))
-        return set_error(SPCONV_E_SHAPE, "rows * ceil(cols / 128) must be below 2^27, cols at most 2^30, strides at most 2^34");
+        return set_error(SPCONV_E_SHAPE, "rows must be below 2^25, rows * ceil(cols / 128) below 2^27, cols at most 2^30, strides at most 2^34");
     const int64_t size = size_of(dtype), size_r = size_of(residual_dtype), size_y = size_of(y_dtype);
     const int64_t size_g = size_of(gain_dtype);
     if (!aligned(x, size) || (residual && !aligned(residual, size_r)) || (total && !aligned(total, size_r)) ||
@@ -163,8 +164,8 @@ spconv_status spconv_quantize_mxfp4(const void *x, spconv_dtype dtype, int64_t l
         return set_error(SPCONV_E_ARG, "x, q or scale is NULL");
     if (ldx < cols)
         return set_error(SPCONV_E_ARG, "ldx must be at least cols");
-    if (cols > (1 << 30) || ldx > kMostStride || rows * static_cast<int64_t>(lines_of(cols)) >= kMostLines)
-        return set_error(SPCONV_E_SHAPE, "rows * ceil(cols / 256) must be below 2^28, cols at most 2^30, ldx at most 2^34");
+    if (cols > (1 << 30) || ldx > kMostStride || rows >= kMostRows || rows * static_cast<int64_t>(lines_of(cols)) >= kMostLines)
+        return set_error(SPCONV_E_SHAPE, "rows must be below 2^25, rows * ceil(cols / 256) below 2^28, cols at most 2^30, ldx at most 2^34");
     if (!aligned(x, size_of(dtype)) || !aligned(q, 16) || !aligned(scale, 16))
         return set_error(SPCONV_E_ARG, "x must be aligned to its element size, q and scale to 16 bytes");
     const Range in[] = {{x, span(rows, cols, ldx, size_of(dtype))}};
@@ -258,7 +259,7 @@ spconv_status spconv_sample_workspace(spconv_dtype dtype, int32_t n, int32_t voc
     *bytes = 0;
     const spconv_status st = check_sample(dtype, n, vocab);
     if (st == SPCONV_OK)
-        *bytes = spconv::sample_workspace(dtype, n, vocab);
+        *bytes = spconv::sample_workspace(n, vocab);
     return st;
 }
 
@@ -284,7 +285,7 @@ spconv_status spconv_sample(const void *logits, spconv_dtype dtype, int64_t ld, 
     if (!aligned(logits, size_of(dtype)) || !aligned(u, 4) || !aligned(temperatures, 4) || !aligned(top_ks, 4) ||
         !aligned(top_ps, 4) || !aligned(min_ps, 4) || !aligned(ids, 4) || !aligned(workspace, 16))
         return set_error(SPCONV_E_ARG, "pointers must be aligned to their element size, the workspace to 16 bytes");
-    const int64_t need = spconv::sample_workspace(dtype, n, vocab), column = n * int64_t(4);
+    const int64_t need = spconv::sample_workspace(n, vocab), column = n * int64_t(4);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return set_error(SPCONV_E_ARG, "the workspace is smaller than spconv_sample_workspace says");
     const Range in[] = {{logits, span(n, vocab, ld, size_of(dtype))}, {u, column}, {temperatures, column},

@@ -72,7 +72,7 @@ struct SampleArgs {
     void *workspace;
 };
 constexpr int32_t kMostTokens = 1 << 20;
-int64_t sample_workspace(int32_t type, int32_t n, int32_t vocab);
+int64_t sample_workspace(int32_t n, int32_t vocab);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t stream);
 
 }  // namespace spconv

@@ -231,6 +231,24 @@ def test_rows_past_32_bit_offsets():
         assert torch.equal(sp.sample(logits, u, **f), sp.sample(logits.contiguous(), u, **f))
 
 
+def test_more_rows_than_a_launch():
+    """Rows past 32768 of more than one chunk, with parameters by row."""
+    import torch
+    n, vocab = 32773, 8200
+    logits = torch.randn((n, vocab), device=device(), generator=torch.Generator(device()).manual_seed(41)).half()
+    u = torch.rand(n, device=device(), generator=torch.Generator(device()).manual_seed(42))
+    t = torch.linspace(0.0, 2.0, n, device=device())
+    k = (torch.arange(n, device=device()) % 7 * 30).int()
+    p = torch.where(torch.arange(n, device=device()) % 3 == 0, 0.9, 1.0)
+    ids = sp.sample(logits, u, t, k, p)
+    for rows in (slice(0, 40), slice(32750, 32773)):
+        some = sample_ref(*(to_numpy(v[rows]) for v in (logits, u, t)), k[rows].cpu().numpy(), to_numpy(p[rows]))
+        assert np.array_equal(ids[rows].cpu().numpy(), some)
+    for f in (dict(), dict(temperature=0.0), dict(top_k=20)):
+        ids = sp.sample(logits, u, **f)
+        assert torch.equal(ids[32700:], sp.sample(logits[32700:], u[32700:], **f))
+
+
 def test_no_rows_and_refusals():
     import torch
     assert sp.sample(torch.empty((0, 9), device=device()), torch.empty(0, device=device())).shape == (0,)

@@ -189,6 +189,30 @@ def test_another_stream(n):
     assert all(torch.equal(o, r) for o, r in zip(outs, ref))
 
 
+@pytest.mark.parametrize("n", [1, 50])
+def test_two_streams_at_once(n):
+    """Chains of calls on two streams, none waiting for the other, each with outputs and workspaces of its own."""
+    import torch
+    note("two streams, %d rows" % n)
+    chains = [_calls(n, 1), _calls(n, 50)]
+    refs = []
+    for step, outs, _, _ in chains:
+        step()
+        torch.cuda.synchronize()
+        refs.append([o.clone() for o in outs])
+        for o in outs:
+            o.zero_()
+    sides = [torch.cuda.Stream() for _ in chains]
+    for side in sides:
+        side.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for (step, _, _, _), side in zip(chains, sides):
+            step(side)
+    torch.cuda.synchronize()
+    for (_, outs, _, _), ref in zip(chains, refs):
+        assert all(torch.equal(o, r) for o, r in zip(outs, ref))
+
+
 @pytest.mark.parametrize("n", [1, 33])
 def test_two_graphs_share_workspaces(n):
     """Graphs of two calls' chains with the same workspaces, replayed in turn on one stream."""

@@ -33,7 +33,7 @@ BAD_NORMS = [
     (dict(dtype="f32", ldx=300, gain_dtype="f32", y_dtype="f32"), S.E_UNSUPPORTED),
     (dict(eps=-1e-6), S.E_ARG), (dict(eps=NAN), S.E_ARG), (dict(eps=INF), S.E_ARG), (dict(ldx=299), S.E_ARG),
     (dict(ldr=299), S.E_ARG), (dict(ldt=299), S.E_ARG), (dict(ldy=299), S.E_ARG),
-    (dict(rows=1 << 26), S.E_SHAPE), (dict(ldx=1 << 40), S.E_SHAPE), (dict(ldr=1 << 40), S.E_SHAPE),
+    (dict(rows=1 << 26), S.E_SHAPE), (dict(rows=1 << 25, cols=64), S.E_SHAPE), (dict(ldx=1 << 40), S.E_SHAPE), (dict(ldr=1 << 40), S.E_SHAPE),
     (dict(ldt=1 << 40), S.E_SHAPE), (dict(ldy=1 << 40), S.E_SHAPE), (dict(x=A + 1), S.E_ARG),
     (dict(residual=B + 1), S.E_ARG), (dict(total=C + 1), S.E_ARG), (dict(gain=D + 1), S.E_ARG),
     (dict(y=E_ + 1), S.E_ARG), (dict(q=F + 8), S.E_ARG), (dict(scale=G + 2), S.E_ARG),
@@ -65,7 +65,7 @@ def _quantize(**kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), S.E_ARG), (dict(q=None), S.E_ARG), (dict(scale=None), S.E_ARG), (dict(rows=-1), S.E_ARG),
     (dict(cols=-1), S.E_ARG), (dict(ldx=299), S.E_ARG), (dict(dtype="fp8"), S.E_ARG), (dict(dtype="mxfp4"), S.E_ARG),
-    (dict(rows=1 << 27, cols=257), S.E_SHAPE), (dict(rows=1, cols=(1 << 30) + 1, ldx=1 << 31), S.E_SHAPE),
+    (dict(rows=1 << 24, cols=4097, ldx=5000), S.E_SHAPE), (dict(rows=1 << 25), S.E_SHAPE), (dict(rows=1, cols=(1 << 30) + 1, ldx=1 << 31), S.E_SHAPE),
     (dict(ldx=1 << 40), S.E_SHAPE), (dict(x=A + 2), S.E_ARG), (dict(q=B + 8), S.E_ARG), (dict(scale=C + 8), S.E_ARG),
     (dict(q=A + 16), S.E_ARG), (dict(scale=B + 64), S.E_ARG), (dict(scale=A + 5 * 300 * 4 - 16), S.E_ARG),
 ])
@@ -90,7 +90,7 @@ def _linear(**kw):
     (dict(n=-1), S.E_ARG), (dict(cin=-1), S.E_ARG), (dict(cout=-1), S.E_ARG), (dict(x_dtype="fp8"), S.E_ARG),
     (dict(y_dtype="mxfp4"), S.E_ARG), (dict(act=3), S.E_ARG), (dict(ldx=299), S.E_ARG), (dict(x_scale=G), S.E_ARG),
     (dict(x_dtype="mxfp4"), S.E_ARG), (dict(cin=0), S.E_SHAPE), (dict(cin=(1 << 22) + 1, ldx=1 << 23), S.E_SHAPE),
-    (dict(n=1 << 26, cin=300, cout=1), S.E_SHAPE), (dict(n=1 << 20, cin=1, cout=1 << 17), S.E_SHAPE),
+    (dict(n=1 << 25, cin=1, cout=1), S.E_SHAPE), (dict(n=1 << 24, cin=2049, ldx=2049, cout=1), S.E_SHAPE), (dict(n=1 << 20, cin=1, cout=1 << 17), S.E_SHAPE),
     (dict(n=1, cin=1 << 22, ldx=1 << 22, cout=1 << 14), S.E_SHAPE), (dict(ldx=1 << 40), S.E_SHAPE),
     (dict(ws=None), S.E_ARG), (dict(size=100), S.E_ARG), (dict(ws=F + 8), S.E_ARG), (dict(w=B + 8), S.E_ARG),
     (dict(w_scale=C + 8), S.E_ARG), (dict(x=A + 1), S.E_ARG), (dict(y=E_ + 1), S.E_ARG), (dict(bias=D + 2), S.E_ARG),
