@@ -27,20 +27,22 @@
 // fill the card; a launch ends where every chunk's part is needed:
 //   A  each chunk's largest key, the largest of each 32 tokens (a segment), and,
 //      where nothing is filtered, the sum of its weights;
-//   B  rows without a filter: the chunk that holds the border, and the token in it.
-//      Few tokens kept (k): the k-th largest of the segments' keys bounds the k-th
-//      largest key from below, so that only the segments above it are read
-//      again.  Else, for all chunks: sums (min_p) or the histogram;
+//   B  where k or p has a border in a bin, or min_p alone is asked for: each chunk's sum (min_p) or
+//      its part of the histogram;
 //   C  each chunk adds up what is above the border's bin and lists what is in it;
-//   D  the border in the list, the chunk, the token.
+//   D  the token, a workgroup a row: without a filter from the chunks' sums; of few kept tokens (k)
+//      from the segments: the k-th largest of their keys bounds the k-th largest key from below, so
+//      that only the segments above it are read again; else from the border in the list and the sums.
+// Calls whose rows all need neither B nor C do without them.  Few kept tokens are D's although A is
+// all that they wait for: in B, 64 x 131072 with parameters by row took 75 us in place of 57.
 // k above 1024 together with p, and longer lists than 8192, go to one workgroup that
 // walks over the whole row.
 //
 // What bounds it.  64 x 131072 in bf16 (16.8 MB, 3.3 us at a copy's rate), on the device alone: t = 0
-// 8.8 us; no filter 23, of it 9 the exponentials (25 64-bit operations each); k = 50 20, of it 10
-// the steps of B, one after the other, each some loads or a few LDS accesses and barriers long (1000
-// to 2500 cycles; k = 500 24); p = 0.9 56: A 6.5, B 16.7 (exponentials and LDS atomics), C 12.9, D
-// 19.7 (the border in 1200 listed tokens 9, the token 5).  One row of 4000: 8.4 to 9.1, with p 13.3.
+// 8.6 us; no filter 21, of it 9 the exponentials (25 64-bit operations each); k = 50 18, of it 10
+// the steps of D, one after the other, each some loads or a few LDS accesses and barriers long (1000
+// to 2500 cycles; k = 500 24); p = 0.9 55: A 6.6, B 15 (exponentials and LDS atomics), C 13, D 20
+// (the border in 1200 listed tokens 9, the token 5).  One row of 4000: 8.4 to 9.1, with p 13.3.
 // Steps one after the other are why a workgroup has 512 threads and not 1024 (each thread's share
 // of such a step is done by twice as many: k = 50 of 4000 took 14 us).  They wait for their own
 // results, not for instructions: the same steps done again at once take nine tenths.
@@ -1126,34 +1128,19 @@ __device__ __forceinline__ void pick_segments(const SampleArgs &a, int32_t row, 
     pick_few(a, row, r, static_cast<int32_t>(sh.count), most, sh);
 }
 
-// B.  Six wavefronts a SIMD are three workgroups a compute unit: with the 97 registers that it would take
-// there are two (64 x 131072 with parameters by row 36.7 us and 32.1; with 64 registers 36.8).
+// B
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 6) sample_rows(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads) sample_sums(SampleArgs a) {
     __shared__ Shared sh;
-    const int32_t row = blockIdx.y, chunk = blockIdx.x, chunks = chunks_of(a.vocab);  // (one workgroup where it does all)
+    const int32_t row = blockIdx.y, chunk = blockIdx.x, chunks = gridDim.x;
     const Row r = row_of(a, row);
-    const bool every = r.mode == kLeast || r.mode == kShare || r.mode == kCount;
-    if (chunk > 0 && !every)
+    if (r.mode != kLeast && r.mode != kShare && r.mode != kCount)
         return;
     const Space s = space_of(a, row);
-    if (r.mode == kFewKept) {
-        pick_segments<T>(a, row, r, s, chunks, sh);
-        return;
-    }
     const uint64_t best = best_of(s, chunks);
-    if (best == 0 || r.mode == kGreedy) {
-        if (chunk == 0 && threadIdx.x == 0)
-            a.ids[row] = best == 0 ? -1 : token_of(best);
+    if (best == 0)
         return;
-    }
     const float most = logit_of(best);
-    if (r.mode == kAll) {
-        pick_all<T>(a, row, r, s, chunks, most, sh);
-        return;
-    }
-    if (r.mode == kDigits)
-        return;
     float v[kPieces][8];
     load_chunk<T>(a, row, chunk, v);
     clear(sh.bins, kBins);
@@ -1250,16 +1237,25 @@ __global__ void __launch_bounds__(kThreads) sample_lists(SampleArgs a) {
 
 // D, a workgroup a row
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_borders(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads) sample_tokens(SampleArgs a) {
     __shared__ Shared sh;
     const int32_t row = blockIdx.x, chunks = chunks_of(a.vocab);
     const Row r = row_of(a, row);
-    if (r.mode == kGreedy || r.mode == kAll || r.mode == kFewKept)
-        return;
     const Space s = space_of(a, row);
-    const uint64_t best = best_of(s, chunks);
-    if (best == 0)
+    if (r.mode == kFewKept) {
+        pick_segments<T>(a, row, r, s, chunks, sh);
         return;
+    }
+    const uint64_t best = best_of(s, chunks);
+    if (best == 0 || r.mode == kGreedy) {
+        if (threadIdx.x == 0)
+            a.ids[row] = best == 0 ? -1 : token_of(best);
+        return;
+    }
+    if (r.mode == kAll) {
+        pick_all<T>(a, row, r, s, chunks, logit_of(best), sh);
+        return;
+    }
     const uint32_t listed = r.mode == kLeast ? 0 : *s.count;
     if (r.mode == kDigits || listed > kList) {
         whole_row<T, false>(a, row, r, sh, nullptr);
@@ -1323,7 +1319,7 @@ hipError_t launch(const SampleArgs &a, hipStream_t stream) {
         sample_short<T><<<a.n, kThreads, 0, stream>>>(a);
         return hipGetLastError();
     }
-    // rows that end in B: a small k, t = 0, no filter
+    // rows that need no sums over all: a small k, t = 0, no filter
     const bool few = !a.top_ks && a.top_k > 0 && few_kept(a.top_k, !a.top_ps && a.top_p < 1);
     const bool greedy = !a.temperatures && !(a.temperature > 0);
     const bool all = !a.top_ks && (a.top_k == 0 || a.top_k >= a.vocab) && !a.top_ps && a.top_p >= 1 && !a.min_ps && !(a.min_p > 0);
@@ -1340,11 +1336,11 @@ hipError_t launch(const SampleArgs &a, hipStream_t stream) {
         part.workspace = static_cast<uint64_t *>(a.workspace) + row * row_words(a.vocab);
         const dim3 grid(chunks, rows);
         sample_chunks<T><<<grid, kSegments, 0, stream>>>(part);
-        sample_rows<T><<<few || greedy || all ? dim3(1, rows) : grid, kThreads, 0, stream>>>(part);
         if (!few && !greedy && !all) {
+            sample_sums<T><<<grid, kThreads, 0, stream>>>(part);
             sample_lists<T><<<grid, kThreads, 0, stream>>>(part);
-            sample_borders<T><<<rows, kThreads, 0, stream>>>(part);
         }
+        sample_tokens<T><<<rows, kThreads, 0, stream>>>(part);
     }
     return hipGetLastError();
 }
