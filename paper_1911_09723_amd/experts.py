@@ -33,7 +33,8 @@ def _bind():
     global _torch, _lib, _device, _raw_stream
     import torch
     _lib = load_library()
-    _device = torch.cuda.current_device
+    # what torch.cuda.current_device asks once the GPU is in use, as it is where a tensor lies there
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if _raw_stream is None:
         def _raw_stream(device):

@@ -36,21 +36,24 @@ def _rows_like(t, shape, device, what: str) -> int:
     return ld if rows > 1 else cols
 
 
-def _norm(x, gain, eps, residual, total, y, q, scale, stream):
-    """Queue the norm of x into the outputs given; returns total (made here where a residual is given)."""
+def _norm(x, gain, eps, residual, total, y, dtype, q, scale, stream):
+    """Queue the norm of x into the outputs given, and into y of `dtype` (x's where None) and total,
+    which are made here where neither y nor q, or a residual without total, is given; returns (y, total)."""
     kind = _type(x.dtype, "x")
     rows, cols, ldx, device = _matrix(x, "x")
-    shape = rows, cols
+    shape, like = (rows, cols), _experts._torch.empty_like  # (rows that lie as x's: contiguous)
     kind_r = kind_g = kind_y = F32
     at_r = at_t = at_g = at_y = None
-    ldr = ldt = ldy = 0
+    ldr = ldt = ldy = cols
     if residual is not None:
         ldr, kind_r, at_r = _rows_like(residual, shape, device, "residual"), _type(residual.dtype, "residual"), residual.data_ptr()
         if total is None:
-            total = _experts._torch.empty_like(residual)  # a fraction of a microsecond less than new_empty
+            total = like(residual)
         elif total.dtype != residual.dtype:
             raise ValueError("total must have the residual's type")
-        ldt, at_t = _rows_like(total, shape, device, "total"), total.data_ptr()
+        else:
+            ldt = _rows_like(total, shape, device, "total")
+        at_t = total.data_ptr()
     elif total is not None:
         raise ValueError("total is the sum with a residual")
     if gain is not None:
@@ -58,13 +61,17 @@ def _norm(x, gain, eps, residual, total, y, q, scale, stream):
         if gain.shape != (cols,) or gain.get_device() != device or not gain.is_contiguous():
             raise ValueError("gain must be a contiguous vector of %d values on GPU %d" % (cols, device))
     if y is not None:
-        ldy, kind_y, at_y = _rows_like(y, shape, device, "y"), _type(y.dtype, "y"), y.data_ptr()
+        ldy, kind_y = _rows_like(y, shape, device, "y"), _type(y.dtype, "y")
+    elif q is None:
+        y, kind_y = (like(x), kind) if dtype is None else (like(x, dtype=dtype), _type(dtype, "dtype"))
+    if y is not None:
+        at_y = y.data_ptr()
     if rows and cols:
         _check(_experts._lib.spconv_rms_norm(
             x.data_ptr(), kind, ldx, at_r, kind_r, ldr, at_t, ldt, at_g, kind_g, eps, at_y, kind_y, ldy,
             None if q is None else q.data_ptr(), None if scale is None else scale.data_ptr(), rows, cols,
             _handle(stream, device)))
-    return total
+    return y, total
 
 
 def rms_norm(x, gain=None, eps: float = 1e-6, residual=None, y=None, dtype=None, total=None, stream=None):
@@ -72,13 +79,10 @@ def rms_norm(x, gain=None, eps: float = 1e-6, residual=None, y=None, dtype=None,
     (or x): a matrix [rows, cols] of ``dtype`` (x's, or float32).  With a residual
     the pair (y, total): total is h in the residual's type, into ``total`` (a new
     tensor, or the residual itself) where given."""
-    _type(x.dtype, "x")
-    if y is None:
-        y = _experts._torch.empty_like(x, dtype=dtype) if dtype else _experts._torch.empty_like(x)
-    elif dtype is not None and y.dtype != dtype:
+    if y is not None and dtype is not None and y.dtype != dtype:
         raise ValueError("y must be of dtype")
-    total = _norm(x, gain, eps, residual, total, y, None, None, stream)
-    return y if residual is None else (y, total)
+    pair = _norm(x, gain, eps, residual, total, y, dtype, None, None, stream)
+    return pair[0] if residual is None else pair
 
 
 def rms_norm_fp8(x, gain=None, eps: float = 1e-6, residual=None, q=None, scale=None, y=None, total=None, stream=None):
@@ -97,7 +101,7 @@ def rms_norm_fp8(x, gain=None, eps: float = 1e-6, residual=None, q=None, scale=N
         scale = x.new_empty((kb, rows), dtype=torch.float32)
     else:
         _given(scale, (kb, rows), torch.float32, x.device, "scale")
-    total = _norm(x, gain, eps, residual, total, y, q, scale, stream)
+    _, total = _norm(x, gain, eps, residual, total, y, None, q, scale, stream)
     return (q, scale) if residual is None else (q, scale, total)
 
 
