@@ -130,6 +130,23 @@ def test_layer_without_norms_is_as_before():
     assert np.array_equal(headed.tokens.cpu().numpy(), sample_ref(to_numpy(out), np.zeros(9), 0.0))
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_layers_whose_norms_are_taken_away(bits):
+    """Without gains the layer's steps are those of its parts, called one by one; and of a layer made without any."""
+    import torch
+    note("layer without norms, %d bits" % bits)
+    layer, x = _layer("bf16", 9, bits, sampler=dict(temperature=0.7, top_k=20)), _draw(9, 320, "bf16", 5)
+    u = _u(9, 6)
+    bare = sp.ExpertLayer(layer.router, layer.experts, 3, 9, torch.bfloat16, layer.head, sampler=layer.sampler)
+    bare.u.copy_(u)
+    out = bare.forward(x).clone()
+    logits = torch.empty((9, 8), device=device())
+    sp.spconv_linear(x.float(), layer.router, None, "none", logits, 9, 320, 8)
+    total = layer.experts.run(x, *sp.route(logits, 3)) + x
+    assert torch.equal(bare.y, total) and torch.equal(out, layer.head.run(total))
+    assert torch.equal(bare.tokens, sp.sample(out, u, 0.7, 20))
+
+
 def test_refusals_of_the_layer():
     import torch
     layer = _layer("bf16", 2, 4)
