@@ -70,6 +70,7 @@ struct SampleArgs {
     int32_t *ids;
     int32_t n, vocab;
     void *workspace;
+    int64_t words;  // set by launch_sample: 8-byte words of the workspace from row to row
 };
 constexpr int32_t kMostTokens = 1 << 20;
 int64_t sample_workspace(int32_t n, int32_t vocab);
