@@ -241,7 +241,10 @@ bool one_round(int32_t lines, int32_t cout, int32_t channels) {
 // Measured (bf16, two launches in brackets): 1 x 1024 -> 1024 3.3 us (4.8), 1 x 4096 -> 4096 5.2
 // (7.0), 1 x 8192 -> 8192 11.0 (13.0), 4 x 4096 -> 8192 7.8 (8.3), 8 x 4096 -> 4096 7.8 (7.4); beyond,
 // 8 x 8192 -> 1024 10.5 (8.8), 16 x 4096 -> 4096 11.2 (7.6), and with more wavefronts than the
-// card holds 1 x 4096 -> 14336 11.9 (10.1).
+// card holds 1 x 4096 -> 14336 11.9 (10.1).  In f32, whose rows take twice the registers (63 of them are
+// spilled above 4096 channels), on the device alone: 1 x 4096 -> 4096 5.9 (6.8), 8 x 4096 -> 4096 8.6 (7.3),
+// 4 x 4096 -> 8192 11.3 (9.0), 1 x 8192 -> 8192 13.8 (11.4): less than the launch that is saved on the host,
+// more than two launches in a graph.
 bool linear4_takes_rows(int32_t n, int32_t cin, int32_t cout) {
     const int32_t lines = lines_of(cin);
     return static_cast<int64_t>(n) * ((lines + kStreamWaves - 1) / kStreamWaves) <= 8 &&

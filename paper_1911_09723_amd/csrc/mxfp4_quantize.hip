@@ -45,7 +45,8 @@ hipError_t rows_of(const void *x, int64_t ldx, int32_t rows, int32_t cols, uint8
     const int32_t lines = lines_of(cols), groups = (rows + 7) / 8;
     const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * sizeof(T) % 16 == 0;
     // Four lines a thread once that still gives every compute unit several workgroups; rows are
-    // then read past the caches (8192 x 4096 in bf16 18.3 us, through them 22.4; 2048 x 4096 6.3 and 7.4).
+    // then read past the caches (8192 x 4096 in bf16 18.3 us, through them 22.4; 2048 x 4096 6.3 and 7.4;
+    // not compared in f32, whose rows are twice the bytes).
     if (static_cast<int64_t>(groups) * lines >= 4096)
         quantize4_rows<T, 4, true><<<groups * ((lines + 3) / 4), 256, 0, stream>>>(static_cast<const T *>(x), ldx, rows, cols, q,
                                                                             scale, lines, groups, wide);

@@ -28,7 +28,8 @@ struct None {};
 // A piece of 16 or 8 bytes, past the caches where `stream`: of a long call little is still there
 // when the next one reads it, and it takes room from what is read.  bf16 with residual and codes,
 // us, through the caches and past them: 8192 x 4096 52.2 and 46.3 (loads kept: 47.9), 2048 x 4096
-// 16.6 and 14.4, 1024 x 4096 9.6 and 10.3.
+// 16.6 and 14.4, 1024 x 4096 9.6 and 10.3.  The other types go by the same bytes of x; they were not
+// compared.
 template <typename V>
 __device__ __forceinline__ void put(V *p, V v, bool stream) {
     if (stream)
@@ -62,7 +63,7 @@ __device__ __forceinline__ void store8(T *p, int left, bool wide, bool stream, c
             p[i] = e.v[i];
 }
 
-// Eight values that are read once, `left` of them there.
+// Eight values, `left` of them there.
 template <typename T>
 __device__ __forceinline__ void read8(const T *p, int left, bool wide, bool stream, float *v) {
     if (stream && wide && left >= 8) {
@@ -191,8 +192,10 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) norm_rows(NormA
     }
 }
 
-// Rows that registers do not hold: read twice.  A thread reads what it writes
-// before it writes it, so total and y may lie where residual and x do.
+// Rows that registers do not hold: read twice, past the caches both times where the call is long (512 x
+// 40000 in bf16 41 us with residual, 4.0 TB/s by what has to move once; the first time through
+// them was not compared).  A thread reads what it writes before it writes it, so total and y may lie
+// where residual and x do.
 template <typename T, typename R, typename W>
 __global__ void __launch_bounds__(1024) norm_long(NormArgs a) {
     __shared__ double part[16];

@@ -36,12 +36,13 @@
 // Calls whose rows all need neither B nor C do without them.  Few kept tokens are D's although A is
 // all that they wait for: in B, 64 x 131072 with parameters by row took 75 us in place of 57.
 // k above 1024 together with p, and longer lists than 8192, go to one workgroup that
-// walks over the whole row.
+// walks over the whole row: a flat row of 131072 or a border among 2^20 tokens whose bin holds so many
+// takes 0.9 and 4.2 ms with p = 0.9.
 //
 // What bounds it.  64 x 131072 in bf16 (16.8 MB, 3.3 us at a copy's rate), on the device alone: t = 0
 // 8.6 us; no filter 21, of it 9 the exponentials (25 64-bit operations each); k = 50 18, of it 10
 // the steps of D, one after the other, each some loads or a few LDS accesses and barriers long (1000
-// to 2500 cycles; k = 500 24); p = 0.9 55: A 6.6, B 15 (exponentials and LDS atomics), C 13, D 20
+// to 2500 cycles; k = 500 31); p = 0.9 55: A 6.6, B 15 (exponentials and LDS atomics), C 13, D 20
 // (the border in 1200 listed tokens 9, the token 5).  One row of 4000: 8.4 to 9.1, with p 13.3.
 // Steps one after the other are why a workgroup has 512 threads and not 1024 (each thread's share
 // of such a step is done by twice as many: k = 50 of 4000 took 14 us).  They wait for their own
@@ -102,9 +103,10 @@ __device__ __forceinline__ void load_logits(const T *p, int left, float *v) {
 
 enum Mode { kGreedy, kAll, kLeast, kFewKept, kShare, kCount, kDigits };
 
-// Whether the first k of a row are listed in LDS.  Alone, more than 512 take less as a histogram
-// (1000 of 131072, one row, 39 us and 99; 256 x 50001 83 and 95); together with a share, a list is
-// what there is but for the walk over the whole row (64 x 131072, k = 2000 and p = 0.9: 336 us).
+// Whether the first k of a row are listed in LDS.  Alone, 1000 take less as a histogram (on the device,
+// one row of 131072 28 us and 83, 256 x 50001 67 and 90), 600 of one row as much (28), of many rows more
+// (256 x 50001 67 and 38).  Together with a share, a list is what there is but for the walk over the
+// whole row (64 x 131072 with p = 0.9: k = 1000 100 us, as a walk 314; k = 2000 330).
 __host__ __device__ __forceinline__ bool few_kept(int32_t k, bool share) { return k <= (share ? kFew : 512); }
 
 // A number that stays in scalar registers: else each use of it would be moved to vector registers.
@@ -154,8 +156,8 @@ __device__ __forceinline__ Row row_of(const SampleArgs &a, int32_t row) {
 }
 
 // A token's weight times 2^42: 2^z with z = (l - m) scale + 42, as 2^n times a polynomial in f = z -
-// n, |f| <= 1/2: the one of degree 9 that agrees with 2^f at 0 and at nine Chebyshev nodes, 3.7e-14
-// off, exact at 0, so that the largest weight is 2^42 and equal logits weigh the same.  n is found
+// n, |f| <= 1/2: the one of degree 9 that agrees with 2^f at nine Chebyshev nodes, of which 0 is one,
+// and at 0 in its slope, too; 3.7e-14 off, exact at 0, so that the largest weight is 2^42.  n is found
 // by an addition whose sum's last place is one.  z is cut off at -960, which is far below what counts.
 __device__ __forceinline__ double weight_of(float l, float most, const Row &r) {
     const double z = fmax(fma(static_cast<double>(l) - static_cast<double>(most), r.scale, r.c.shift), r.c.least);
@@ -820,7 +822,7 @@ __device__ __forceinline__ void whole_row(const SampleArgs &a, int32_t row, cons
 }
 
 // Rows that LDS holds.  What bounds it are the steps, one after the other: some microseconds a
-// row, 256 rows at a time.
+// row, 512 rows at a time (62 KB of LDS and 79 registers: two workgroups a compute unit).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_short(SampleArgs a) {
     __shared__ OneRow sh;
@@ -871,7 +873,7 @@ __global__ void __launch_bounds__(kSegments) sample_chunks(SampleArgs a) {
     if (best) {
         const float most = logit_of(best);
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {  // moves, as registers take no index (read again 25.6 us in place of 23.5, 256 x 50001)
+        for (int j = 0; j < 4; ++j) {  // moves, as registers take no index (A of 256 x 50001 23.5 us, reading again 25.6)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const Sum u = units(weight_of(v[0][e], most, r), r);
