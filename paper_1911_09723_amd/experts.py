@@ -9,6 +9,9 @@ Work is queued on ``stream`` (a torch stream; default: torch's current one).
 With another stream than the current one pass the outputs and the workspace
 too: torch may hand memory that it allocates here to the current stream's work
 before the other stream is done with it.
+
+Forward only: nothing here has a gradient.  Inputs that require one are taken as
+they are, and what is computed from them is cut off from them, as by ``detach``.
 """
 
 from __future__ import annotations

@@ -3,8 +3,8 @@
 The arithmetic runs in libspconv's kernels (include/spconv.h says what each
 computes and how its arrays are laid out); this module checks shapes, types and
 strides, allocates what a call writes with torch's allocator and passes
-addresses on, as ``experts.py`` does.  What that module says about streams holds
-here, too.
+addresses on, as ``experts.py`` does.  What that module says about streams and
+gradients holds here, too.
 """
 
 from __future__ import annotations

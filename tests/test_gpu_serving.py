@@ -160,6 +160,18 @@ def test_refusals_of_the_layer():
             sp.ExpertLayer(*args, layer.head, head_norm=bad)
 
 
+def test_results_carry_no_gradient():
+    """Inputs that require one are taken as they are; what comes out is cut off from them."""
+    import torch
+    x, gain = _draw(4, 256, "f32", 1).requires_grad_(), _draw(1, 256, "f32", 2)[0].requires_grad_()
+    y, total = sp.rms_norm(x, gain, residual=x)
+    head = sp.Mxfp4Linear.from_dense(_draw(300, 256, "f32", 3).requires_grad_())
+    out = head.run(x)
+    outs = (y, total, *sp.rms_norm_fp8(x, gain), *sp.quantize_mxfp4(x), out, sp.sample(x, _u(4, 4)))
+    assert not any(o.requires_grad for o in outs)
+    assert torch.equal(out, head.run(x.detach())) and torch.equal(y, sp.rms_norm(x.detach(), gain.detach(), residual=x.detach())[0])
+
+
 def _calls(n, seed, spaces=None):
     """(a chain of every operator's calls with all that they write given, its outputs, its input, its workspaces)."""
     import torch
